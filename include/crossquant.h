@@ -12,7 +12,7 @@
  *   - Every pointer is a DEVICE pointer owned by the caller; the library allocates nothing,
  *     frees nothing and never synchronises with the host.  `stream` is a hipStream_t passed as
  *     void* (NULL = the default stream).  All work is enqueued on that stream, in order.
- *   - X and W are IEEE binary16, row-major.  Outputs are fully overwritten; vectors that the
+ *   - X and W are IEEE binary16, row-major (calls that take a cq_type: that type).  Outputs are fully overwritten; vectors that the
  *     kernels accumulate into (t, c, zero_count) are cleared on the stream inside the call.
  *   - Return value: CQ_OK (0) or a negative cq_status.  Argument errors, sizes over a limit and
  *     unsupported requests are found on the host before anything is enqueued: such a return means
@@ -42,8 +42,12 @@ typedef enum {
     CQ_ERR_ALIGN = -5,       /* a pointer violates the stated alignment */
     CQ_ERR_UNSUPPORTED = -6, /* valid request this build does not implement */
     CQ_ERR_HIP = -7,         /* a kernel launch failed (hipGetLastError) */
-    CQ_ERR_ALIAS = -8        /* an output vector overlaps an input vector it must not overlap */
+    CQ_ERR_ALIAS = -8,       /* an output vector overlaps an input vector it must not overlap */
+    CQ_ERR_TYPE = -9         /* an element type is not one of cq_type */
 } cq_status;
+
+/* Element types of the calls that take one (the FP8 and cache calls; all others are binary16). */
+typedef enum { CQ_F16 = 0, CQ_BF16 = 1 } cq_type;
 
 /* Upper limits on sizes (keeps every index in 32 bits inside the kernels). */
 #define CQ_MAX_DIM ((int64_t)1 << 24)        /* T, I, O, leading dimensions */
@@ -303,6 +307,91 @@ int crossquant_quantize_fp6(const void *X, int64_t T, int64_t I, int64_t ldx, co
 int crossquant_w4a4_linear(const void *qx_fp6, const float *row_scale, const void *qw_fp6,
                            const float *w_scale, int64_t T, int64_t I, int64_t O, void *Y, int64_t ldy,
                            int32_t *acc_debug, void *stream);
+
+/*
+ * FP8 (e4m3) linear layer with a binary32 scale for every block of 128, and the two calls that make its operands.
+ *
+ * A group of activations is 128 consecutive channels of one token, a block of weights 128 input x 128 output channels; the
+ * last ones of a matrix are shorter.  With m = max |x| over the group:
+ *   m < 2^-100: s = r = 0;  else s = fl32(m / 448), r = fl32(448 / m);   code = e4m3(fl32(x * r)), the nearest, ties to even
+ * (an element that is not finite makes its group's scale infinite or NaN, and with it the outputs of its token).
+ * Ip = 128 ceil(I / 128): rows of codes are padded with zeros to whole groups, so that the linear has whole blocks.
+ *
+ * crossquant_quantize_fp8: X [T][ldx] of type x_type, any layout (16-byte aligned with ldx % 8 == 0 and I % 8 == 0 runs fastest).
+ *   codes: out, e4m3 [T][Ip], 16-byte aligned.  scale: out, float [Ip / 128][T] (a block's scales of all tokens are neighbours).
+ * crossquant_weight_quantize_fp8: W [I][O] of type w_type.
+ *   qw: out, e4m3 [O][Ip], 16-byte aligned.  w_scale: out, float [ceil(O / 128)][Ip / 128].
+ * crossquant_fp8_linear: I is the codes' row length, a multiple of 128 (else CQ_ERR_UNSUPPORTED).  qx: e4m3 [T][I], qw: e4m3 [O][I], both 16-byte
+ *   aligned; x_scale: float [I / 128][T]; w_scale: float [ceil(O / 128)][I / 128].
+ *   Y_ik = sum_b fl32(x_scale[b][i] w_scale[k / 128][b]) P_b,  P_b = sum over the 128 channels of block b of qx_ij qw_kj,
+ *   in binary32, rounded once to y_type (within P_b the matrix instruction sums 8 neighbouring products with 13 bits below the
+ *   largest one's exponent, and drops the rest); Y: out [T][ldy], ldy >= O.  The order of the sum over b depends on T, I and O
+ *   alone: equal calls give equal bits.
+ */
+int crossquant_quantize_fp8(const void *X, int x_type, int64_t T, int64_t I, int64_t ldx, void *codes, float *scale, void *stream);
+int crossquant_weight_quantize_fp8(const void *W, int w_type, int64_t I, int64_t O, void *qw, float *w_scale, void *stream);
+int crossquant_fp8_linear(const void *qx, const float *x_scale, const void *qw, const float *w_scale, int64_t T, int64_t I,
+                          int64_t O, void *Y, int y_type, int64_t ldy, void *stream);
+
+/*
+ * Key/value cache held in CrossQuant codes.  Keys and values are activations: a token's row of a head, `dim` channels, is quantized
+ * when it is written with the CrossQuant step of that row, its own maximum and calibrated column factors,
+ *   a = fl32(t^alpha / q_max), t = max |x|;  D_j = fl32(a b_j);  q_j = D_j == 0 ? 0 : clamp(rne(fl32(x_j / D_j)), +-q_max)
+ * and stands for fl32(q_j D_j) from then on (q_max = 127 or 7).  b_j = c_j^(1-alpha) is what crossquant_quantize gives as col_scale for
+ * calibration keys (or values) laid out as [tokens][heads * dim] with the same alpha; without column factors (NULL: all 1) alpha = 1, the
+ * per-token step, is the sensible one.
+ *
+ * The cache is `pages` pages of page_size places.  Place `slot` is place slot % page_size of page slot / page_size.
+ *   k_codes, v_codes: bits 8: int8 [pages][heads][page_size][dim]; bits 4: packed nibbles [pages][heads][page_size][dim / 2], even
+ *     column in the low nibble.  16-byte aligned.  k_scale, v_scale: float [pages][heads][page_size], the rows' factors a.
+ *   k_col, v_col: nullable, float [heads][dim], 16-byte aligned: the column factors b.
+ *   dim is 64, 128 or 256; page_size a power of two from 16 to 65536 (else CQ_ERR_UNSUPPORTED); pages * page_size < 2^31.
+ */
+typedef struct {
+    void *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+    const float *k_col, *v_col;
+    int64_t pages, page_size, heads, dim;
+    int64_t bits;
+    double alpha;
+} cq_cache;
+
+/*
+ * Quantizes keys and values K, V [T][heads][dim] (type `type`; token i's row of head h starts at i * token_stride + h * head_stride
+ * elements; 16-byte aligned with strides that are multiples of 8, else CQ_ERR_ALIGN) into the places slots[i], int32 [T].
+ * A slot that is negative or past the cache writes nothing (padding tokens).  No other place is touched.
+ * A slot may occur once in a call: of several tokens with the same slot, what the place holds afterwards is undefined.
+ */
+int crossquant_cache_write(const cq_cache *cache, const void *K, int64_t k_token_stride, int64_t k_head_stride, const void *V,
+                           int64_t v_token_stride, int64_t v_head_stride, int type, const int32_t *slots, int64_t T, void *stream);
+
+/*
+ * The keys and values of the places slots[i], int32 [T], in any order and as often as wanted: K, V out, [T][heads][dim] of type
+ * `type`, contiguous, 16-byte aligned, the values fl32(q D) rounded once more to the type.  Rows of a slot that is negative or past the cache are zero.
+ */
+int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T, void *K, void *V, int type, void *stream);
+
+/*
+ * Attention of the last S tokens of B sequences over the cache (decode: S = 1, or a few drafted tokens), whose keys and values are
+ * in the cache already:
+ *   out[b][s][h] = sum_p softmax_p(scale * q . k_p) v_p over the positions p < min(lengths[b] - (S - 1 - s), max_length)
+ * with k_p, v_p of head h / (q_heads / heads) in binary32 from the codes.  Position p of sequence b is place p % page_size of page
+ * page_table[b][p / page_size].  A row that sees no position (lengths[b] too small) is zero.  Positions on a page that is negative or past the
+ * cache are not seen, and entries of the table behind the last visible position are not read; so are codes and scales there.
+ * Q, out: type `type`; Q: token s of sequence b at b * q_batch_stride + s * q_token_stride, head h another h * q_head_stride
+ *   elements on (16-byte aligned, strides multiples of 8, else CQ_ERR_ALIGN); out: [B][S][q_heads][dim], contiguous, 16-byte aligned.
+ * q_heads: a multiple of the cache's heads.  page_table: int32 [B][table_width]; lengths: int32 [B].
+ * max_length: no visible position is at or past it (1 .. table_width * page_size): what a launch is sized for.
+ * workspace: crossquant_cache_attention_workspace(...) bytes, 16-byte aligned (0 bytes: may be NULL), for this call alone until it is done: calls that
+ *   may overlap, and graphs that may, take one each.  Need not be cleared.
+ * Queries enter the product as 16-bit fixed-point numbers relative to their row's largest |q_j b_j| (at most 1.6e-5 of it off), codes as they
+ * are; scores, softmax statistics and sums are binary32, the weights of the values binary16 relative to the largest.
+ */
+int64_t crossquant_cache_attention_workspace(const cq_cache *cache, int64_t B, int64_t S, int64_t q_heads, int64_t max_length);
+int crossquant_cache_attention(const cq_cache *cache, const void *Q, int64_t q_batch_stride, int64_t q_token_stride,
+                               int64_t q_head_stride, int type, int64_t B, int64_t S, int64_t q_heads, const int32_t *page_table,
+                               int64_t table_width, const int32_t *lengths, int64_t max_length, float scale, void *out,
+                               void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *crossquant_status_string(int status);

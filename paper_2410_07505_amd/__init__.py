@@ -16,6 +16,8 @@ _EXPORTS = (
     "crossquant_kernel_analysis", "crossquant_kernel_analysis_static", "crossquant_kernel_count", "crossquant_pack_fp6", "crossquant_pack_fp6_weights", "crossquant_w4a4_linear",
     "crossquant_quantize", "crossquant_quantize_batched", "crossquant_quantize_fp6", "crossquant_quantize_linear_fused", "crossquant_status_string", "crossquant_unpack_int4", "crossquant_version", "crossquant_w8a8_linear",
     "crossquant_weight_quantize", "crossquant_weight_quantize_grouped", "lib", "raw",
+    "crossquant_quantize_fp8", "crossquant_weight_quantize_fp8", "crossquant_fp8_linear", "CrossQuantCache", "crossquant_cache",
+    "crossquant_cache_write", "crossquant_cache_read", "crossquant_cache_attention", "crossquant_cache_attention_workspace",
 )
 __all__ = list(_EXPORTS)
 

@@ -59,6 +59,24 @@ lib.crossquant_w8a8_linear.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp
 lib.crossquant_quantize_linear_fused.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _f32, _int, _vp, _vp, _i64, _vp, _i64, _vp,
                                                  _vp, _vp, _vp]
 lib.crossquant_quantize_linear_fused.restype = _int
+lib.crossquant_quantize_fp8.argtypes = [_vp, _int, _i64, _i64, _i64, _vp, _vp, _vp]
+lib.crossquant_weight_quantize_fp8.argtypes = [_vp, _int, _i64, _i64, _vp, _vp, _vp]
+lib.crossquant_fp8_linear.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]
+
+
+class _CacheStruct(ctypes.Structure):                 # cq_cache
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scale", _vp), ("v_scale", _vp), ("k_col", _vp), ("v_col", _vp),
+                ("pages", _i64), ("page_size", _i64), ("heads", _i64), ("dim", _i64), ("bits", _i64), ("alpha", ctypes.c_double)]
+
+
+lib.crossquant_cache_write.argtypes = [_vp, _vp, _i64, _i64, _vp, _i64, _i64, _int, _vp, _i64, _vp]
+lib.crossquant_cache_read.argtypes = [_vp, _vp, _i64, _vp, _vp, _int, _vp]
+lib.crossquant_cache_attention_workspace.argtypes = [_vp, _i64, _i64, _i64, _i64]
+lib.crossquant_cache_attention_workspace.restype = _i64
+lib.crossquant_cache_attention.argtypes = [_vp, _vp, _i64, _i64, _i64, _int, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _vp, _i64, _vp]
+for _n in ("crossquant_quantize_fp8", "crossquant_weight_quantize_fp8", "crossquant_fp8_linear", "crossquant_cache_write",
+           "crossquant_cache_read", "crossquant_cache_attention"):
+    getattr(lib, _n).restype = _int
 for _n in ("crossquant_absmax", "crossquant_quantize", "crossquant_absmax_quantize", "crossquant_absmax_batched",
            "crossquant_quantize_batched", "crossquant_calib_read", "crossquant_calib_copy", "crossquant_calib_mfma_i8", "crossquant_pack_fp6",
            "crossquant_w4a4_linear", "crossquant_quantize_fp6", "crossquant_kernel_count", "crossquant_kernel_analysis", "crossquant_unpack_int4",
@@ -730,3 +748,269 @@ def crossquant_quantize_linear_fused(X: torch.Tensor, t: torch.Tensor, c: torch.
                                                 Y.stride(0), row_scale.data_ptr(), col_scale.data_ptr(),
                                                 _ptr(acc_debug), _stream(X)))
     return Y, row_scale, col_scale, acc_debug
+
+
+# ---- FP8 codes with a scale for every block of 128, and the key/value cache: binary16 or bfloat16 ----
+
+_TYPES = {torch.float16: 0, torch.bfloat16: 1}        # cq_type
+_fp8 = torch.float8_e4m3fn
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _type(dtype, name: str) -> int:
+    code = _TYPES.get(dtype)
+    if code is None:
+        raise TypeError("%s must be float16 or bfloat16, not %s" % (name, dtype))
+    return code
+
+
+def _launch(call, like: torch.Tensor, *args) -> None:
+    """The call on the current stream of like's device, with that device current."""
+    index = like.get_device()
+    if index < 0:
+        raise ValueError("the tensors must be on a GPU")
+    if index == _current_device():
+        status = call(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = call(*args, _raw_stream(index))
+    if status != 0:
+        raise CrossQuantError(status)
+
+
+def crossquant_quantize_fp8(X: torch.Tensor, *, codes: torch.Tensor = None, scale: torch.Tensor = None):
+    """e4m3 codes of X (float16 or bfloat16 [T][I]) with a scale for every 128 channels of a token.
+
+    Returns (codes [T][Ip], scale float32 [Ip / 128][T]); Ip is I up to a multiple of 128, the codes past I are zero."""
+    if not isinstance(X, torch.Tensor):
+        raise TypeError("X must be a torch.Tensor")
+    kind = _type(X.dtype, "X")
+    _matrix(X, X.dtype, "X")
+    T, I = X.shape
+    blocks = (I + 127) // 128
+    if codes is None:
+        codes = torch.empty((T, 128 * blocks), dtype=_fp8, device=X.device)
+    else:
+        _buf(codes, _fp8, (T, 128 * blocks), "codes", X)
+    if scale is None:
+        scale = torch.empty((blocks, T), dtype=torch.float32, device=X.device)
+    else:
+        _buf(scale, torch.float32, (blocks, T), "scale", X)
+    _on_gpu(X, "X")
+    _launch(lib.crossquant_quantize_fp8, X, X.data_ptr(), kind, T, I, X.stride(0) if T > 1 else I, codes.data_ptr(), scale.data_ptr())
+    return codes, scale
+
+
+def crossquant_weight_quantize_fp8(W: torch.Tensor, *, qw: torch.Tensor = None, w_scale: torch.Tensor = None):
+    """e4m3 codes of a weight W (float16 or bfloat16 [I][O]) with a scale for every block of 128 x 128.
+
+    Returns (qw [O][Ip], w_scale float32 [ceil(O / 128)][Ip / 128]); Ip is I up to a multiple of 128."""
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise TypeError("W must be a 2-D tensor")
+    kind = _type(W.dtype, "W")
+    if not W.is_contiguous():
+        raise ValueError("W must be contiguous")
+    I, O = W.shape
+    blocks, out_blocks = (I + 127) // 128, (O + 127) // 128
+    if qw is None:
+        qw = torch.empty((O, 128 * blocks), dtype=_fp8, device=W.device)
+    else:
+        _buf(qw, _fp8, (O, 128 * blocks), "qw", W)
+    if w_scale is None:
+        w_scale = torch.empty((out_blocks, blocks), dtype=torch.float32, device=W.device)
+    else:
+        _buf(w_scale, torch.float32, (out_blocks, blocks), "w_scale", W)
+    _on_gpu(W, "W")
+    _launch(lib.crossquant_weight_quantize_fp8, W, W.data_ptr(), kind, I, O, qw.data_ptr(), w_scale.data_ptr())
+    return qw, w_scale
+
+
+def crossquant_fp8_linear(qx: torch.Tensor, x_scale: torch.Tensor, qw: torch.Tensor, w_scale: torch.Tensor, *,
+                          dtype: torch.dtype = None, Y: torch.Tensor = None) -> torch.Tensor:
+    """Y = X . W on e4m3 codes with block scales.  qx [T][I], x_scale float32 [I / 128][T], qw [O][I], w_scale float32
+    [ceil(O / 128)][I / 128], I a multiple of 128 (crossquant_quantize_fp8 and crossquant_weight_quantize_fp8 pad to one).
+    dtype: of the result, float16 (without Y the default) or bfloat16; Y: the result's buffer, rows may be padded."""
+    _matrix(qx, _fp8, "qx")
+    _matrix(qw, _fp8, "qw")
+    if not qx.is_contiguous() or not qw.is_contiguous():
+        raise ValueError("qx and qw must be contiguous")
+    T, I = qx.shape
+    O, I2 = qw.shape
+    if I != I2:
+        raise ValueError("qx is [T][I] and qw [O][I]: the contraction lengths differ (%d, %d)" % (I, I2))
+    if I % 128:
+        raise CrossQuantError(-6)
+    if qw.device != qx.device:
+        raise ValueError("qw must be on %s" % qx.device)
+    _buf(x_scale, torch.float32, (I // 128, T), "x_scale", qx)
+    _buf(w_scale, torch.float32, ((O + 127) // 128, I // 128), "w_scale", qx)
+    if Y is None:
+        kind = _type(dtype if dtype is not None else torch.float16, "dtype")
+        Y = torch.empty((T, O), dtype=dtype if dtype is not None else torch.float16, device=qx.device)
+        ldy = O
+    else:
+        if not isinstance(Y, torch.Tensor) or tuple(Y.shape) != (T, O) or (dtype is not None and Y.dtype != dtype):
+            raise ValueError("Y must be a tensor of shape (%d, %d) and the dtype asked for" % (T, O))
+        kind = _type(Y.dtype, "Y")
+        if (O > 1 and Y.stride(1) != 1) or (T > 1 and Y.stride(0) < O) or Y.device != qx.device:
+            raise ValueError("Y must have unit stride inside a row, non-overlapping rows, and be on %s" % qx.device)
+        ldy = Y.stride(0) if T > 1 else O
+    _on_gpu(qx, "qx")
+    _launch(lib.crossquant_fp8_linear, qx, qx.data_ptr(), x_scale.data_ptr(), qw.data_ptr(), w_scale.data_ptr(), T, I, O,
+            Y.data_ptr(), kind, ldy)
+    return Y
+
+
+class CrossQuantCache:
+    """A key/value cache of CrossQuant codes: what crossquant_cache returns and the cache calls take.  It keeps the tensors it was
+    made of (k_codes, k_scale, v_codes, v_scale, k_col, v_col), which stay the caller's to read, copy or clear."""
+
+    __slots__ = ("k_codes", "k_scale", "v_codes", "v_scale", "k_col", "v_col", "bits", "alpha", "pages", "page_size", "heads", "dim",
+                 "_struct", "_address")
+
+
+def crossquant_cache(k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torch.Tensor, v_scale: torch.Tensor, bits: int, *,
+                     alpha: float = 1.0, k_col: torch.Tensor = None, v_col: torch.Tensor = None) -> CrossQuantCache:
+    """The cache made of these tensors.  k_codes, v_codes: int8 [pages][heads][page_size][dim] (bits 8) or uint8
+    [pages][heads][page_size][dim / 2] (bits 4); k_scale, v_scale: float32 [pages][heads][page_size]; k_col, v_col: float32
+    [heads][dim], the column factors (col_scale of crossquant_quantize for calibration keys and values with the same alpha).
+    A place that has not been written holds what the tensors held."""
+    if bits not in (4, 8):
+        raise CrossQuantError(-3)
+    if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
+        raise TypeError("k_codes must be a 4-D tensor")
+    pages, heads, page_size, row = k_codes.shape
+    dim = row if bits == 8 else 2 * row
+    code_type = torch.int8 if bits == 8 else torch.uint8
+    _buf(k_codes, code_type, (pages, heads, page_size, row), "k_codes", k_codes)
+    _buf(v_codes, code_type, (pages, heads, page_size, row), "v_codes", k_codes)
+    _buf(k_scale, torch.float32, (pages, heads, page_size), "k_scale", k_codes)
+    _buf(v_scale, torch.float32, (pages, heads, page_size), "v_scale", k_codes)
+    if k_col is not None:
+        _buf(k_col, torch.float32, (heads, dim), "k_col", k_codes)
+    if v_col is not None:
+        _buf(v_col, torch.float32, (heads, dim), "v_col", k_codes)
+    if not 0.0 <= alpha <= 1.0:
+        raise CrossQuantError(-4)
+    c = CrossQuantCache()
+    c.k_codes, c.k_scale, c.v_codes, c.v_scale, c.k_col, c.v_col = k_codes, k_scale, v_codes, v_scale, k_col, v_col
+    c.bits, c.alpha, c.pages, c.page_size, c.heads, c.dim = bits, float(alpha), pages, page_size, heads, dim
+    c._struct = _CacheStruct(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(k_col), _ptr(v_col),
+                             pages, page_size, heads, dim, bits, alpha)
+    c._address = ctypes.addressof(c._struct)
+    return c
+
+
+def _cache(cache) -> torch.Tensor:
+    if not isinstance(cache, CrossQuantCache):
+        raise TypeError("cache must come from crossquant_cache")
+    return cache.k_codes
+
+
+def _rows(ten, shape, dtype, name: str, like: torch.Tensor):
+    """A tensor whose rows of the last axis are contiguous; the strides of the axes before it (0 where an axis has one place)."""
+    if not isinstance(ten, torch.Tensor) or ten.dtype != dtype:
+        raise TypeError("%s must be a tensor of dtype %s" % (name, dtype))
+    if tuple(ten.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(ten.shape)))
+    if ten.stride(-1) != 1 or ten.device != like.device:
+        raise ValueError("%s must have unit stride along its last axis and be on %s" % (name, like.device))
+    return [s if n > 1 else 0 for s, n in zip(ten.stride()[:-1], shape)]
+
+
+def _slots(slots, like: torch.Tensor) -> int:
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+        raise TypeError("slots must be a 1-D int32 tensor")
+    T = slots.shape[0]
+    _buf(slots, torch.int32, (T,), "slots", like)
+    return T
+
+
+def crossquant_cache_write(cache: CrossQuantCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantizes keys and values (float16 or bfloat16 [T][heads][dim], rows may be strided) into the places slots (int32 [T]):
+    place s % page_size of page s / page_size.  Slots that are negative or past the cache write nothing; a slot may occur once."""
+    like = _cache(cache)
+    T = _slots(slots, like)
+    if not isinstance(K, torch.Tensor):
+        raise TypeError("K must be a torch.Tensor")
+    kind = _type(K.dtype, "K")
+    shape = (T, cache.heads, cache.dim)
+    kt, kh = _rows(K, shape, K.dtype, "K", like)
+    vt, vh = _rows(V, shape, K.dtype, "V", like)
+    _on_gpu(like, "the cache")
+    _launch(lib.crossquant_cache_write, like, cache._address, K.data_ptr(), kt, kh, V.data_ptr(), vt, vh, kind, slots.data_ptr(), T)
+
+
+def crossquant_cache_read(cache: CrossQuantCache, slots: torch.Tensor, *, dtype: torch.dtype = None, K: torch.Tensor = None,
+                          V: torch.Tensor = None):
+    """Keys and values of the places slots (int32 [T]) as float16 (without K and V the default) or bfloat16 [T][heads][dim]; rows of slots that are
+    negative or past the cache are zero.  Returns (K, V)."""
+    like = _cache(cache)
+    T = _slots(slots, like)
+    if dtype is None:
+        dtype = K.dtype if isinstance(K, torch.Tensor) else V.dtype if isinstance(V, torch.Tensor) else torch.float16
+    kind = _type(dtype, "dtype")
+    shape = (T, cache.heads, cache.dim)
+    if K is None:
+        K = torch.empty(shape, dtype=dtype, device=like.device)
+    else:
+        _buf(K, dtype, shape, "K", like)
+    if V is None:
+        V = torch.empty(shape, dtype=dtype, device=like.device)
+    else:
+        _buf(V, dtype, shape, "V", like)
+    _on_gpu(like, "the cache")
+    _launch(lib.crossquant_cache_read, like, cache._address, slots.data_ptr(), T, K.data_ptr(), V.data_ptr(), kind)
+    return K, V
+
+
+def crossquant_cache_attention_workspace(cache: CrossQuantCache, B: int, S: int, q_heads: int, max_length: int) -> int:
+    """Bytes of workspace that crossquant_cache_attention needs for these sizes (0: none)."""
+    _cache(cache)
+    n = int(lib.crossquant_cache_attention_workspace(cache._address, B, S, q_heads, max_length))
+    if n < 0:
+        raise CrossQuantError(-2)
+    return n
+
+
+def crossquant_cache_attention(cache: CrossQuantCache, Q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *,
+                               scale: float = None, max_length: int = None, out: torch.Tensor = None,
+                               workspace: torch.Tensor = None) -> torch.Tensor:
+    """Attention of the last S tokens of B sequences over the cache, which holds their keys and values already.
+
+    Q: float16 or bfloat16 [B][S][q_heads][dim] (rows may be strided); page_table: int32 [B][width], lengths: int32 [B].  Token s of
+    sequence b sees its positions below lengths[b] - (S - 1 - s); a row that sees none is zero.  scale: of the scores, 1 / sqrt(dim)
+    without it; max_length: a bound on the lengths that the launch is sized for (all the table holds without it).  workspace:
+    uint8, at least crossquant_cache_attention_workspace(...) bytes, for this call until it is done (one is allocated without it)."""
+    like = _cache(cache)
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 4:
+        raise TypeError("Q must be a 4-D tensor")
+    kind = _type(Q.dtype, "Q")
+    B, S, q_heads, dim = Q.shape
+    if dim != cache.dim or q_heads % cache.heads:
+        raise ValueError("Q must be [B][S][q_heads][%d] with q_heads a multiple of %d" % (cache.dim, cache.heads))
+    qb, qs, qh = _rows(Q, (B, S, q_heads, dim), Q.dtype, "Q", like)
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise TypeError("page_table must be a 2-D int32 tensor")
+    width = page_table.shape[1]
+    _buf(page_table, torch.int32, (B, width), "page_table", like)
+    _buf(lengths, torch.int32, (B,), "lengths", like)
+    if max_length is None:
+        max_length = width * cache.page_size
+    if out is None:
+        out = torch.empty((B, S, q_heads, dim), dtype=Q.dtype, device=like.device)
+    else:
+        _buf(out, Q.dtype, (B, S, q_heads, dim), "out", like)
+    _on_gpu(like, "the cache")
+    if workspace is None:
+        need = int(lib.crossquant_cache_attention_workspace(cache._address, B, S, q_heads, max_length))
+        if need > 0:                                  # (negative: the call below says what is wrong)
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        have = max(need, 0)
+    else:
+        have = workspace.numel() if isinstance(workspace, torch.Tensor) else 0
+        _buf(workspace, torch.uint8, (have,), "workspace", like)
+    _launch(lib.crossquant_cache_attention, like, cache._address, Q.data_ptr(), qb, qs, qh, kind, B, S, q_heads,
+            page_table.data_ptr(), width, lengths.data_ptr(), max_length, dim ** -0.5 if scale is None else scale, out.data_ptr(),
+            _ptr(workspace), have)
+    return out

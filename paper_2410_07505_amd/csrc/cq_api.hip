@@ -50,6 +50,49 @@ inline int from_hip(hipError_t e) {
     return e == hipSuccess ? CQ_OK : (e == hipErrorInvalidValue ? CQ_ERR_SHAPE : CQ_ERR_HIP);
 }
 
+inline bool type_ok(int type) { return type == CQ_F16 || type == CQ_BF16; }
+
+// what every cache call asks of the descriptor
+int check_cache(const cq_cache* c, cq::CacheView& view) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return CQ_ERR_NULL;
+    if (!dim_ok(c->pages) || !dim_ok(c->heads) || c->page_size < 1 || c->dim < 1) return CQ_ERR_SHAPE;
+    if (c->bits != 4 && c->bits != 8) return CQ_ERR_BITS;
+    if (!(c->alpha >= 0.0 && c->alpha <= 1.0)) return CQ_ERR_ALPHA;
+    if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0) return CQ_ERR_UNSUPPORTED;
+    if (c->dim != 64 && c->dim != 128 && c->dim != 256) return CQ_ERR_UNSUPPORTED;
+    const int64_t places = c->pages * c->page_size;                      // below 2^40
+    if (places >= (int64_t)1 << 31 || places * c->heads > CQ_MAX_ELEMS || places * c->heads * c->dim > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16) ||
+        !aligned(c->k_col, 16) || !aligned(c->v_col, 16))
+        return CQ_ERR_ALIGN;
+    view.k_codes = static_cast<uint8_t*>(c->k_codes);
+    view.v_codes = static_cast<uint8_t*>(c->v_codes);
+    view.k_scale = c->k_scale;
+    view.v_scale = c->v_scale;
+    view.k_col = c->k_col;
+    view.v_col = c->v_col;
+    view.pages = c->pages;
+    view.page_shift = __builtin_ctzll((unsigned long long)c->page_size);
+    view.heads = (int)c->heads;
+    view.dim = (int)c->dim;
+    view.bits = (int)c->bits;
+    view.alpha = c->alpha;
+    return CQ_OK;
+}
+
+// a stride between rows of `dim` elements that 16-byte loads can follow
+int check_row_stride(int64_t stride) {
+    if (stride < 0 || stride > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    return stride % 8 == 0 ? CQ_OK : CQ_ERR_ALIGN;
+}
+
+// B, S, q_heads and max_length of an attention call
+int check_attention(const cq::CacheView& c, int64_t B, int64_t S, int64_t q_heads, int64_t max_length) {
+    if (!dim_ok(B) || !dim_ok(S) || !dim_ok(q_heads) || q_heads % c.heads != 0) return CQ_ERR_SHAPE;
+    if (S * q_heads > CQ_MAX_DIM || B * S * q_heads > (int64_t)1 << 31 || B * S * q_heads * c.dim > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    return max_length >= 1 && max_length < (int64_t)1 << 31 ? CQ_OK : CQ_ERR_SHAPE;
+}
+
 }  // namespace
 
 extern "C" {
@@ -315,6 +358,93 @@ int crossquant_w4a4_linear(const void* qx_fp6, const float* row_scale, const voi
                                            static_cast<hipStream_t>(stream)));
 }
 
+int crossquant_quantize_fp8(const void* X, int x_type, int64_t T, int64_t I, int64_t ldx, void* codes, float* scale, void* stream) {
+    if (!codes || !scale) return CQ_ERR_NULL;
+    if (int s = check_matrix(X, T, I, ldx)) return s;
+    if (!type_ok(x_type)) return CQ_ERR_TYPE;
+    if (!aligned(codes, 16) || !aligned(scale, 4)) return CQ_ERR_ALIGN;
+    return from_hip(cq::launch_quantize_fp8(static_cast<const uint16_t*>(X), x_type == CQ_BF16, (int)T, (int)I, ldx,
+                                            static_cast<uint8_t*>(codes), scale, static_cast<hipStream_t>(stream)));
+}
+
+int crossquant_weight_quantize_fp8(const void* W, int w_type, int64_t I, int64_t O, void* qw, float* w_scale, void* stream) {
+    if (!qw || !w_scale) return CQ_ERR_NULL;
+    if (int s = check_matrix(W, I, O, O)) return s;
+    if (!type_ok(w_type)) return CQ_ERR_TYPE;
+    if (!aligned(qw, 16) || !aligned(w_scale, 4)) return CQ_ERR_ALIGN;
+    return from_hip(cq::launch_weight_quantize_fp8(static_cast<const uint16_t*>(W), w_type == CQ_BF16, (int)I, (int)O,
+                                                   static_cast<uint8_t*>(qw), w_scale, static_cast<hipStream_t>(stream)));
+}
+
+int crossquant_fp8_linear(const void* qx, const float* x_scale, const void* qw, const float* w_scale, int64_t T, int64_t I,
+                          int64_t O, void* Y, int y_type, int64_t ldy, void* stream) {
+    if (!qx || !x_scale || !qw || !w_scale || !Y) return CQ_ERR_NULL;
+    if (!dim_ok(T) || !dim_ok(I) || !dim_ok(O) || ldy < O || ldy > CQ_MAX_DIM) return CQ_ERR_SHAPE;
+    if (T * O > CQ_MAX_ELEMS || T * ldy > CQ_MAX_ELEMS || T * I > CQ_MAX_ELEMS || I * O > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    if (!type_ok(y_type)) return CQ_ERR_TYPE;
+    if (!aligned(qx, 16) || !aligned(qw, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(Y, 2)) return CQ_ERR_ALIGN;
+    if (I % 128 != 0) return CQ_ERR_UNSUPPORTED;
+    return from_hip(cq::launch_fp8_linear(qx, x_scale, qw, w_scale, (int)T, (int)I, (int)O, static_cast<uint16_t*>(Y),
+                                          y_type == CQ_BF16, ldy, static_cast<hipStream_t>(stream)));
+}
+
+int crossquant_cache_write(const cq_cache* cache, const void* K, int64_t k_token_stride, int64_t k_head_stride, const void* V,
+                           int64_t v_token_stride, int64_t v_head_stride, int type, const int32_t* slots, int64_t T, void* stream) {
+    if (!K || !V || !slots) return CQ_ERR_NULL;
+    cq::CacheView view;
+    if (int s = check_cache(cache, view)) return s;
+    if (!dim_ok(T)) return CQ_ERR_SHAPE;
+    if (!type_ok(type)) return CQ_ERR_TYPE;
+    if (!aligned(K, 16) || !aligned(V, 16) || !aligned(slots, 4)) return CQ_ERR_ALIGN;
+    for (int64_t stride : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
+        if (int s = check_row_stride(stride)) return s;
+    return from_hip(cq::launch_cache_write(view, static_cast<const uint16_t*>(K), k_token_stride, k_head_stride,
+                                           static_cast<const uint16_t*>(V), v_token_stride, v_head_stride, type == CQ_BF16, slots,
+                                           (int)T, static_cast<hipStream_t>(stream)));
+}
+
+int crossquant_cache_read(const cq_cache* cache, const int32_t* slots, int64_t T, void* K, void* V, int type, void* stream) {
+    if (!K || !V || !slots) return CQ_ERR_NULL;
+    cq::CacheView view;
+    if (int s = check_cache(cache, view)) return s;
+    if (!dim_ok(T) || T * view.heads * view.dim > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    if (!type_ok(type)) return CQ_ERR_TYPE;
+    if (!aligned(K, 16) || !aligned(V, 16) || !aligned(slots, 4)) return CQ_ERR_ALIGN;
+    return from_hip(cq::launch_cache_read(view, slots, (int)T, static_cast<uint16_t*>(K), static_cast<uint16_t*>(V), type == CQ_BF16,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+int64_t crossquant_cache_attention_workspace(const cq_cache* cache, int64_t B, int64_t S, int64_t q_heads, int64_t max_length) {
+    cq::CacheView view;
+    if (check_cache(cache, view) != CQ_OK || check_attention(view, B, S, q_heads, max_length) != CQ_OK) return -1;
+    return cq::cache_attention_workspace(view, {B, (int)S, (int)q_heads, (int)max_length});
+}
+
+int crossquant_cache_attention(const cq_cache* cache, const void* Q, int64_t q_batch_stride, int64_t q_token_stride,
+                               int64_t q_head_stride, int type, int64_t B, int64_t S, int64_t q_heads, const int32_t* page_table,
+                               int64_t table_width, const int32_t* lengths, int64_t max_length, float scale, void* out,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!Q || !page_table || !lengths || !out) return CQ_ERR_NULL;
+    cq::CacheView view;
+    if (int s = check_cache(cache, view)) return s;
+    if (int s = check_attention(view, B, S, q_heads, max_length)) return s;
+    if (!dim_ok(table_width) || max_length > table_width << view.page_shift || B * table_width > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    if (!std::isfinite(scale)) return CQ_ERR_SHAPE;
+    if (!type_ok(type)) return CQ_ERR_TYPE;
+    if (!aligned(Q, 16) || !aligned(out, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(workspace, 16))
+        return CQ_ERR_ALIGN;
+    for (int64_t stride : {q_batch_stride, q_token_stride, q_head_stride})
+        if (int s = check_row_stride(stride)) return s;
+    const cq::AttentionShape shape = {B, (int)S, (int)q_heads, (int)max_length};
+    const int64_t need = cq::cache_attention_workspace(view, shape);
+    if (need > 0 && !workspace) return CQ_ERR_NULL;
+    if (workspace_bytes < need) return CQ_ERR_SHAPE;
+    return from_hip(cq::launch_cache_attention(view, shape, static_cast<const uint16_t*>(Q), q_batch_stride, q_token_stride,
+                                               q_head_stride, type == CQ_BF16, page_table, table_width, lengths, scale,
+                                               static_cast<uint16_t*>(out), static_cast<float*>(workspace),
+                                               static_cast<hipStream_t>(stream)));
+}
+
 int crossquant_calib_read(const void* src, int64_t bytes, unsigned long long* sink, void* stream) {
     if (!src) return CQ_ERR_NULL;
     if (bytes < 16 || bytes % 16 != 0) return CQ_ERR_SHAPE;
@@ -353,6 +483,7 @@ const char* crossquant_status_string(int status) {
         case CQ_ERR_UNSUPPORTED: return "unsupported request";
         case CQ_ERR_HIP: return "kernel launch failed";
         case CQ_ERR_ALIAS: return "an output vector overlaps an input vector";
+        case CQ_ERR_TYPE: return "element type must be binary16 or bfloat16";
         default: return "unknown status";
     }
 }

@@ -158,6 +158,36 @@ hipError_t launch_pack_fp6(const void* codes, int src_format, bool weights, int 
 hipError_t launch_w4a4_linear(const void* qx6, const float* row_scale, const void* qw6, const float* w_scale, int T,
                               int I, int O, uint16_t* Y, int64_t ldy, int32_t* acc_debug, hipStream_t stream);
 
+// FP8 codes with a scale for every block of 128, and the linear layer on them (I: whole blocks).
+hipError_t launch_quantize_fp8(const uint16_t* X, bool bf16, int T, int I, int64_t ldx, uint8_t* codes, float* scale,
+                               hipStream_t stream);
+hipError_t launch_weight_quantize_fp8(const uint16_t* W, bool bf16, int I, int O, uint8_t* qw, float* w_scale, hipStream_t stream);
+hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* qw, const float* w_scale, int T, int I, int O,
+                             uint16_t* Y, bool bf16, int64_t ldy, hipStream_t stream);
+
+// The key/value cache (crossquant.h: cq_cache); places = pages << page_shift < 2^31.
+struct CacheView {
+    uint8_t *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+    const float *k_col, *v_col;
+    int64_t pages;
+    int page_shift, heads, dim, bits;
+    double alpha;
+};
+hipError_t launch_cache_write(const CacheView& c, const uint16_t* K, int64_t k_token, int64_t k_head, const uint16_t* V,
+                              int64_t v_token, int64_t v_head, bool bf16, const int32_t* slots, int T, hipStream_t stream);
+hipError_t launch_cache_read(const CacheView& c, const int32_t* slots, int T, uint16_t* K, uint16_t* V, bool bf16,
+                             hipStream_t stream);
+// Attention over it (crossquant.h: crossquant_cache_attention); what the launch needs as workspace (bytes).
+struct AttentionShape {
+    int64_t B;
+    int S, q_heads, max_length;
+};
+int64_t cache_attention_workspace(const CacheView& c, const AttentionShape& a);
+hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& a, const uint16_t* Q, int64_t q_batch, int64_t q_token,
+                                  int64_t q_head, bool bf16, const int32_t* table, int64_t table_width, const int32_t* lengths,
+                                  float scale, uint16_t* out, float* workspace, hipStream_t stream);
+
 // Roofline calibration (plain read, plain copy, MFMA-only loop); bytes is a multiple of 16.
 hipError_t launch_calib_read(const void* src, int64_t bytes, unsigned long long* sink, hipStream_t stream);
 hipError_t launch_calib_copy(const void* src, void* dst, int64_t bytes, hipStream_t stream);
