@@ -18,6 +18,7 @@
 // LDS row 16 ni + i of a wave's weight rows holds its channel 4 NT (i >> 2) + 4 ni + (i & 3): a lane's 4 NT outputs of a token
 // are neighbours in Y.
 #include <algorithm>
+#include <type_traits>
 
 #include "cq_gemm_common.h"
 
@@ -27,6 +28,23 @@ namespace {
 __device__ __forceinline__ v4f product128(const v8i& w, const v8i& x) {
     // formats 0 = e4m3; scale operands 0 select the unscaled instruction
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, v4f{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+}
+
+// a wave-uniform pointer, in scalar registers whatever the compiler made of it
+__device__ __forceinline__ const void* in_scalar(const void* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);      // (the builtin's int would extend its sign)
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+    return reinterpret_cast<const void*>((uint64_t)hi << 32 | lo);
+}
+// request_1k and request_words from a scalar base and a lane's 32-bit offset
+__device__ __forceinline__ void request_1k_from(const void* base, uint32_t off, const int8_t* dst) {
+    const uint32_t lds_off = (uint32_t)(uintptr_t)((lptr_t)dst);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 sc0" : : "v"(off), "s"(in_scalar(base)), "s"(lds_off) : "m0");
+}
+__device__ __forceinline__ void request_words_from(const void* base, uint32_t off, const int8_t* dst) {
+    const uint32_t lds_off = (uint32_t)(uintptr_t)((lptr_t)dst);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(in_scalar(base)), "s"(lds_off) : "m0");
 }
 
 template <bool BF16>
@@ -201,6 +219,227 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
     }
 }
 
+// Large layers: 256 x 256 tiles, one share of the contraction, held to a schedule by hand.
+//
+// A wave's 128 tokens x 64 channels are multiplied token tile by token tile.  While the four products of tile mi run, those of tile
+// mi - 1 are added to their totals (the vector unit needs half the matrix unit's time for that) and the fragment of tile mi + 1 is
+// read.  A step's one barrier stands before its last tile: by then every wave has read all it needs of this step, so its place in
+// LDS is free, and what the next step needs has to have landed.  The last tile's products cover the barrier and, weight tile by
+// weight tile as they are done with, the reads of the next step's weight fragments.
+//
+// What costs time beside the matrix unit are the requests: a CU's vector memory unit takes 16 clocks for each (1 KiB), and a wave
+// stands still while its own waits there.  So every wave makes one request a token tile, 8 a step, evenly over the step, which
+// leaves the ones made last little time to land: LDS holds nearly three steps of activations beside two of weights, and the
+// requests of the first half of a step are for the next step, those of the second half for the one after that.
+//   weights: two slots of 32 KiB;
+//   activations: a ring of 92 pieces of 1 KiB (8 rows), 32 a step: pieces 0 .. 27 of step k + 3 and 28 .. 31 of step k + 2 take the
+//     place of step k's.  Waves 0-3 request three of the former and one of the latter, waves 4-7 four of the former;
+//   token scales: three slots of 1 KiB.
+// Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us, two a product 857,
+// this form KRING us.
+constexpr int kRingTile = 256, kHalf = 128 * 128;
+constexpr int kRingB = 5 * kHalf, kRingScales = kRingB + 2 * 2 * kHalf, kRingLds = kRingScales + 3 * 1024;
+static_assert(kRingLds <= 160 * 1024, "LDS of a CU");
+
+template <bool BF16>
+__global__ void __launch_bounds__(64 * kSplitWaves, 2)
+gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
+                     const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
+                     int tiles_n, bool vec) {
+    constexpr int MT = 8, NT = 4, WN = 4, kMidAt = 0, kLateAt = 4, kEarlyAt = 1;
+    extern __shared__ __align__(16) int8_t lds[];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int fr = lane & 15, grp = lane >> 4;
+    const int64_t K = (int64_t)nk * 128;
+
+    int tile_m, tile_n;
+    if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, tile_m, tile_n)) return;
+    const int m0 = tile_m * kRingTile, n0 = tile_n * kRingTile;
+
+    // ---- requests.  A lane's offsets from the tile's first row of the operand: below 2^32 (256 rows of fewer than 2^24 bytes).
+    const int8_t* const a_base = qx + (int64_t)m0 * K;
+    const int8_t* const b_base = qw + (int64_t)n0 * K;
+    // waves 0-3 ("front") request the weights and the scales, waves 4-7 the activations: eight pieces a step each
+    const bool front = wave < 4;
+    uint32_t from[8];                                         // waves 4-7: four pieces of either half
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int w = wave & 3, R = (front ? 64 * w + 8 * i : 128 * (i >> 2) + 32 * w + 8 * (i & 3)) + (lane >> 3);
+        const int in = R % 64, j = in & 15;
+        const uint32_t row = (uint32_t)(front ? min(R - in + 16 * (j >> 2) + 4 * (in >> 4) + (j & 3), O - 1 - n0) : min(R, T - 1 - m0));
+        from[i] = row * (uint32_t)K + ((lane & 7) ^ ((R >> 1) & 7)) * 16;
+    }
+    // the scales of 64 tokens a front wave: word 8 f + mi of a 128-token half is the one of its token 16 mi + f (one past the last
+    // token reads the last one's)
+    const uint32_t s_from = (uint32_t)min(128 * ((wave & 3) >> 1) + 16 * (lane & 7) + 8 * (wave & 1) + (lane >> 3), T - 1 - m0) * 4;
+    auto request_a = [&](int half, int k, int slot) {         // half of the activations of step k
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            request_1k_from(a_base + (int64_t)k * 128, from[4 * half + i], lds + slot * kHalf + (4 * (wave & 3) + i) * 1024);
+    };
+    auto request_b = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            request_1k_from(b_base + (int64_t)k * 128, from[i], lds + kRingB + (k & 1) * 2 * kHalf + (8 * (wave & 3) + i) * 1024);
+    };
+    auto request_scales = [&](int k, int slot) {
+        request_words_from(x_scale + m0 + (int64_t)min(k, nk - 1) * T, s_from, lds + kRingScales + slot * 1024 + (wave & 3) * 256);
+    };
+
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NT; ++ni) acc[mi][ni] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const float* ws_row = n0 + wn * 64 < O ? w_scale + (int64_t)((n0 + wn * 64) / 128) * nk : w_scale;
+    float ws_all = ws_row[min(lane, nk - 1)];                 // the weight block's scales of 64 steps
+
+    // step 0, then what earlier steps would have requested
+    if (front) {
+        request_scales(0, 0);
+        request_b(0);
+        if (nk > 1) {
+            request_scales(1, 1);
+            request_scales(2, 2);
+            request_b(1);
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(10, 0));
+        } else {
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+        }
+    } else {
+        request_a(0, 0, 0);
+        request_a(1, 0, 1);
+        if (nk > 1) {
+            request_a(0, 1, 2);
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(4, 0));
+        } else {
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+        }
+    }
+    step_barrier();
+
+    const int sw = (grp ^ ((fr >> 1) & 7)) * 16;
+    const int8_t* a_lo = lds + wm * kHalf + fr * 128 + sw;
+    const int8_t* a_hi = lds + wm * kHalf + fr * 128 + (sw ^ 64);
+    const int8_t* b_lo = lds + kRingB + (wn * 64 + fr) * 128 + sw;
+    const int8_t* b_hi = lds + kRingB + (wn * 64 + fr) * 128 + (sw ^ 64);
+    const int8_t* s_at = lds + kRingScales + wm * 512 + fr * 32;
+    int b_turn = 2 * kHalf;                                   // to the other slot
+    int slot_a = wm;                                          // the wave's half of the step whose fragments are read: 2 k + wm mod 5
+    int slot_next = 3;                                        // 2 k + 3 mod 5: the second half of step k + 1
+    int slot_s = 0;
+    auto two = [](const int8_t* lo, const int8_t* hi) {
+        return __builtin_shufflevector(*reinterpret_cast<const v4i*>(lo), *reinterpret_cast<const v4i*>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    v8i b[NT], a[4];
+    v4f p[4], s[2], s_next[2];                                // (scales of the step's eight token tiles, and the next step's)
+#pragma unroll
+    for (int ni = 0; ni < NT; ++ni) b[ni] = two(b_lo + ni * 2048, b_hi + ni * 2048);
+#pragma unroll
+    for (int mi = 0; mi < 2; ++mi) {
+        a[mi] = two(a_lo + mi * 2048, a_hi + mi * 2048);
+        s[mi] = *reinterpret_cast<const v4f*>(s_at + mi * 16);
+        s_next[mi] = s[mi];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_all), 0));
+    float s_old = 0.0f;                                       // scale of the products of the tile before
+
+    // next_c: there is a step after k; more_c: and one after that
+    auto step = [&](auto next_c, auto more_c, int k) {
+        constexpr bool kNext = decltype(next_c)::value, kMore = decltype(more_c)::value;
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+            if (mi == MT - 2) {
+                // all of step k + 1 has landed (its requests are older than this step's seven for k + 2), and nobody reads step k
+                // any more
+                if (kMore && !front) __builtin_amdgcn_s_waitcnt(waitcnt_imm(4, 0));
+                else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+                step_barrier();
+                const int turn_a = slot_a >= 3 ? -3 * kHalf : 2 * kHalf;
+                slot_a += slot_a >= 3 ? -3 : 2;
+                a_lo += turn_a;
+                a_hi += turn_a;
+                b_lo += b_turn;
+                b_hi += b_turn;
+                b_turn = -b_turn;
+                const int turn_s = slot_s == 2 ? -2048 : 1024;
+                s_at += turn_s;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s_next[i] = *reinterpret_cast<const v4f*>(s_at + i * 16);
+            }
+            // the fragment after the next one (past the last step: what is there, not used)
+            constexpr int kTile = 16 * 128;
+            const int ahead = (mi + 2) % MT;
+            a[(mi + 2) & 3] = two(a_lo + ahead * kTile, a_hi + ahead * kTile);
+            const float s_now = s[mi >> 2][mi & 3] * ws;
+#pragma unroll
+            for (int ni = 0; ni < NT; ++ni) {
+                // the products of the tile before go to their totals, this tile's take their registers
+                const int mo = mi == 0 ? MT - 1 : mi - 1;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[mo][ni][r] = __builtin_fmaf(p[ni][r], s_old, acc[mo][ni][r]);
+                asm volatile("" : "+v"(acc[mo][ni]));         // (the compiler would move all additions to the step's end)
+                p[ni] = product128(b[ni], a[mi & 3]);
+                if (mi == MT - 1) b[ni] = two(b_lo + ni * 2048, b_hi + ni * 2048);
+                __builtin_amdgcn_sched_barrier(0);
+                if (mi == kMidAt && ni == 0 && kNext && !front) request_a(1, k + 1, slot_next);
+                if (mi == kLateAt && ni == 0 && kMore && !front) request_a(0, k + 2, slot_next == 4 ? 0 : slot_next + 1);
+                if (mi == MT - 2 && ni == kEarlyAt && kMore && front) {
+                    request_scales(k + 3, slot_s);            // step k's place
+                    request_b(k + 2);
+                }
+                if ((mi == kMidAt && ni == 0) || (mi == kLateAt && ni == 0) || (mi == MT - 2 && ni == kEarlyAt)) __builtin_amdgcn_sched_barrier(0);
+            }
+            s_old = s_now;
+        }
+        slot_s = slot_s == 2 ? 0 : slot_s + 1;
+        slot_next += slot_next >= 3 ? -3 : 2;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[i] = s_next[i];
+        const int nx = (k + 1) & 63;
+        if (nx == 0) ws_all = ws_row[min(k + 1 + lane, nk - 1)];
+        ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_all), nx));
+    };
+    for (int k = 0; k < nk - 2; ++k) step(std::true_type(), std::true_type(), k);
+    if (nk > 1) step(std::true_type(), std::false_type(), nk - 2);
+    step(std::false_type(), std::false_type(), nk - 1);       // (waits for every request: none outlives the block)
+#pragma unroll
+    for (int ni = 0; ni < NT; ++ni)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[MT - 1][ni][r] = __builtin_fmaf(p[ni][r], s_old, acc[MT - 1][ni][r]);
+
+    const int col0 = n0 + wn * 64 + 16 * grp, row0 = m0 + wm * 128 + fr;
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi) {
+        const int row = row0 + 16 * mi;
+        if (row >= T) continue;
+        uint16_t* y = Y + (int64_t)row * ldy;
+#pragma unroll
+        for (int ni = 0; ni < NT; ++ni) store4<BF16>(y, col0 + 4 * ni, O, acc[mi][ni], vec);
+    }
+}
+
+hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const float* ws, int T, int nk, int O, uint16_t* Y, bool bf16,
+                   int64_t ldy, hipStream_t stream) {
+    const int tiles_m = (T + kRingTile - 1) / kRingTile, tiles_n = (O + kRingTile - 1) / kRingTile;
+    const int64_t total = (int64_t)tiles_m * tiles_n, blocks = (total + kXcds - 1) / kXcds * kXcds;
+    if (!grid_fits(blocks, 64 * kSplitWaves)) return hipErrorInvalidValue;
+    const bool vec = reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0;
+    static std::atomic<uint64_t> done[2];
+    auto launch = [&](auto k, std::atomic<uint64_t>& d) {
+        if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kRingLds, d); e != hipSuccess) return e;
+        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, vec);
+        return hipGetLastError();
+    };
+    return bf16 ? launch(gemm_fp8_ring_kernel<true>, done[1]) : launch(gemm_fp8_ring_kernel<false>, done[0]);
+}
+
 template <int MT, int NT, int WM, int WN, int WK, int S>
 hipError_t go(const int8_t* qx, const float* xs, const int8_t* qw, const float* ws, int T, int nk, int O, uint16_t* Y, bool bf16,
               int64_t ldy, hipStream_t stream) {
@@ -231,7 +470,7 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
     if (T <= 16) return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
     if (T <= 128) return go<2, 2, 1, 2, 4, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
     if ((int64_t)T * O < 256 * 256 * 200) return go<4, 4, 2, 2, 2, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    return go<8, 4, 2, 4, 1, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+    return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
 }
 
 }  // namespace cq
