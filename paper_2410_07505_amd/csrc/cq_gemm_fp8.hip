@@ -237,26 +237,22 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
 //   token scales: three slots of 1 KiB.
 // Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us, two a product 857,
 // this form KRING us.
+//
+// NT = 2 is half a tile, 256 x 128 (128 x 32 a wave, half the weight requests): outputs of less than a round of the CUs, and the last
+// round of others, are covered by such where that leaves fewer CUs idle (launch_fp8_ring).
 constexpr int kRingTile = 256, kHalf = 128 * 128;
 constexpr int kRingB = 5 * kHalf, kRingScales = kRingB + 2 * 2 * kHalf, kRingLds = kRingScales + 3 * 1024;
 static_assert(kRingLds <= 160 * 1024, "LDS of a CU");
 
-template <bool BF16>
-__global__ void __launch_bounds__(64 * kSplitWaves, 2)
-gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
-                     const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
-                     int tiles_n, bool vec) {
-    constexpr int MT = 8, NT = 4, WN = 4, kMidAt = 0, kLateAt = 4, kEarlyAt = 1;
-    extern __shared__ __align__(16) int8_t lds[];
-
+template <int NT, bool BF16>
+__device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const float* __restrict__ x_scale,
+                                          const int8_t* __restrict__ qw, const float* __restrict__ w_scale, int T, int nk, int O,
+                                          uint16_t* __restrict__ Y, int64_t ldy, bool vec, int8_t* lds, int m0, int n0) {
+    constexpr int MT = 8, WN = 4, WTN = 16 * NT, kMidAt = 0, kLateAt = 3, kEarlyAt = 1, kAhead = 3;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int fr = lane & 15, grp = lane >> 4;
     const int64_t K = (int64_t)nk * 128;
-
-    int tile_m, tile_n;
-    if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, tile_m, tile_n)) return;
-    const int m0 = tile_m * kRingTile, n0 = tile_n * kRingTile;
 
     // ---- requests.  A lane's offsets from the tile's first row of the operand: below 2^32 (256 rows of fewer than 2^24 bytes).
     const int8_t* const a_base = qx + (int64_t)m0 * K;
@@ -266,9 +262,9 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     uint32_t from[8];                                         // waves 4-7: four pieces of either half
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int w = wave & 3, R = (front ? 64 * w + 8 * i : 128 * (i >> 2) + 32 * w + 8 * (i & 3)) + (lane >> 3);
-        const int in = R % 64, j = in & 15;
-        const uint32_t row = (uint32_t)(front ? min(R - in + 16 * (j >> 2) + 4 * (in >> 4) + (j & 3), O - 1 - n0) : min(R, T - 1 - m0));
+        const int w = wave & 3, R = (front ? WTN * w + 8 * i : 128 * (i >> 2) + 32 * w + 8 * (i & 3)) + (lane >> 3);
+        const int in = R % WTN, j = in & 15;
+        const uint32_t row = (uint32_t)(front ? min(R - in + 4 * NT * (j >> 2) + 4 * (in >> 4) + (j & 3), O - 1 - n0) : min(R, T - 1 - m0));
         from[i] = row * (uint32_t)K + ((lane & 7) ^ ((R >> 1) & 7)) * 16;
     }
     // the scales of 64 tokens a front wave: word 8 f + mi of a 128-token half is the one of its token 16 mi + f (one past the last
@@ -281,8 +277,8 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     };
     auto request_b = [&](int k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            request_1k_from(b_base + (int64_t)k * 128, from[i], lds + kRingB + (k & 1) * 2 * kHalf + (8 * (wave & 3) + i) * 1024);
+        for (int i = 0; i < 2 * NT; ++i)
+            request_1k_from(b_base + (int64_t)k * 128, from[i], lds + kRingB + (k & 1) * 2 * kHalf + (2 * NT * (wave & 3) + i) * 1024);
     };
     auto request_scales = [&](int k, int slot) {
         request_words_from(x_scale + m0 + (int64_t)min(k, nk - 1) * T, s_from, lds + kRingScales + slot * 1024 + (wave & 3) * 256);
@@ -294,7 +290,7 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
 #pragma unroll
         for (int ni = 0; ni < NT; ++ni) acc[mi][ni] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const float* ws_row = n0 + wn * 64 < O ? w_scale + (int64_t)((n0 + wn * 64) / 128) * nk : w_scale;
+    const float* ws_row = n0 + wn * WTN < O ? w_scale + (int64_t)((n0 + wn * WTN) / 128) * nk : w_scale;
     float ws_all = ws_row[min(lane, nk - 1)];                 // the weight block's scales of 64 steps
 
     // step 0, then what earlier steps would have requested
@@ -305,7 +301,7 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
             request_scales(1, 1);
             request_scales(2, 2);
             request_b(1);
-            __builtin_amdgcn_s_waitcnt(waitcnt_imm(10, 0));
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * NT + 2, 0));
         } else {
             __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
         }
@@ -324,8 +320,8 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     const int sw = (grp ^ ((fr >> 1) & 7)) * 16;
     const int8_t* a_lo = lds + wm * kHalf + fr * 128 + sw;
     const int8_t* a_hi = lds + wm * kHalf + fr * 128 + (sw ^ 64);
-    const int8_t* b_lo = lds + kRingB + (wn * 64 + fr) * 128 + sw;
-    const int8_t* b_hi = lds + kRingB + (wn * 64 + fr) * 128 + (sw ^ 64);
+    const int8_t* b_lo = lds + kRingB + (wn * WTN + fr) * 128 + sw;
+    const int8_t* b_hi = lds + kRingB + (wn * WTN + fr) * 128 + (sw ^ 64);
     const int8_t* s_at = lds + kRingScales + wm * 512 + fr * 32;
     int b_turn = 2 * kHalf;                                   // to the other slot
     int slot_a = wm;                                          // the wave's half of the step whose fragments are read: 2 k + wm mod 5
@@ -340,11 +336,9 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
 #pragma unroll
     for (int ni = 0; ni < NT; ++ni) b[ni] = two(b_lo + ni * 2048, b_hi + ni * 2048);
 #pragma unroll
-    for (int mi = 0; mi < 2; ++mi) {
-        a[mi] = two(a_lo + mi * 2048, a_hi + mi * 2048);
-        s[mi] = *reinterpret_cast<const v4f*>(s_at + mi * 16);
-        s_next[mi] = s[mi];
-    }
+    for (int mi = 0; mi < kAhead; ++mi) a[mi] = two(a_lo + mi * 2048, a_hi + mi * 2048);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) s_next[i] = s[i] = *reinterpret_cast<const v4f*>(s_at + i * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_all), 0));
@@ -355,7 +349,7 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
         constexpr bool kNext = decltype(next_c)::value, kMore = decltype(more_c)::value;
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
-            if (mi == MT - 2) {
+            if (mi == MT - kAhead) {
                 // all of step k + 1 has landed (its requests are older than this step's seven for k + 2), and nobody reads step k
                 // any more
                 if (kMore && !front) __builtin_amdgcn_s_waitcnt(waitcnt_imm(4, 0));
@@ -375,8 +369,8 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
             }
             // the fragment after the next one (past the last step: what is there, not used)
             constexpr int kTile = 16 * 128;
-            const int ahead = (mi + 2) % MT;
-            a[(mi + 2) & 3] = two(a_lo + ahead * kTile, a_hi + ahead * kTile);
+            const int ahead = (mi + kAhead) % MT;
+            a[(mi + kAhead) & 3] = two(a_lo + ahead * kTile, a_hi + ahead * kTile);
             const float s_now = s[mi >> 2][mi & 3] * ws;
 #pragma unroll
             for (int ni = 0; ni < NT; ++ni) {
@@ -390,11 +384,11 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
                 __builtin_amdgcn_sched_barrier(0);
                 if (mi == kMidAt && ni == 0 && kNext && !front) request_a(1, k + 1, slot_next);
                 if (mi == kLateAt && ni == 0 && kMore && !front) request_a(0, k + 2, slot_next == 4 ? 0 : slot_next + 1);
-                if (mi == MT - 2 && ni == kEarlyAt && kMore && front) {
+                if (mi == MT - kAhead && ni == kEarlyAt && kMore && front) {
                     request_scales(k + 3, slot_s);            // step k's place
                     request_b(k + 2);
                 }
-                if ((mi == kMidAt && ni == 0) || (mi == kLateAt && ni == 0) || (mi == MT - 2 && ni == kEarlyAt)) __builtin_amdgcn_sched_barrier(0);
+                if ((mi == kMidAt && ni == 0) || (mi == kLateAt && ni == 0) || (mi == MT - kAhead && ni == kEarlyAt)) __builtin_amdgcn_sched_barrier(0);
             }
             s_old = s_now;
         }
@@ -414,7 +408,7 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[MT - 1][ni][r] = __builtin_fmaf(p[ni][r], s_old, acc[MT - 1][ni][r]);
 
-    const int col0 = n0 + wn * 64 + 16 * grp, row0 = m0 + wm * 128 + fr;
+    const int col0 = n0 + wn * WTN + 4 * NT * grp, row0 = m0 + wm * 128 + fr;
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
         const int row = row0 + 16 * mi;
@@ -425,16 +419,39 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     }
 }
 
+// The first n_whole tiles of the walk are whole (a multiple of 8, or all there are), the others two halves each, on blocks behind theirs.
+template <bool BF16>
+__global__ void __launch_bounds__(64 * kSplitWaves, 2)
+gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
+                     const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
+                     int tiles_n, int n_whole, bool vec) {
+    extern __shared__ __align__(16) int8_t lds[];
+    const int whole_blocks = (n_whole + kXcds - 1) / kXcds * kXcds;
+    const bool whole = (int)blockIdx.x < whole_blocks;
+    const int block = whole ? blockIdx.x : blockIdx.x - whole_blocks, n = whole ? n_whole : 2 * (tiles_m * tiles_n - n_whole);
+    const int per_xcd = (n + kXcds - 1) / kXcds, at = (block % kXcds) * per_xcd + block / kXcds;    // (see tile_of_block)
+    if (at >= n || block / kXcds >= per_xcd) return;
+    int tile_m, tile_n;
+    tile_of_index(whole ? at : n_whole + at / 2, tiles_m, tiles_n, tile_m, tile_n);
+    const int m0 = tile_m * kRingTile, n0 = tile_n * kRingTile + (whole ? 0 : at % 2 * (kRingTile / 2));
+    if (n0 >= O) return;                                      // the right half of a last tile may have no channel
+    if (whole) ring_tile<4, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, lds, m0, n0);
+    else ring_tile<2, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, lds, m0, n0);
+}
+
 hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const float* ws, int T, int nk, int O, uint16_t* Y, bool bf16,
-                   int64_t ldy, hipStream_t stream) {
+                   int64_t ldy, int n_cu, hipStream_t stream) {
     const int tiles_m = (T + kRingTile - 1) / kRingTile, tiles_n = (O + kRingTile - 1) / kRingTile;
-    const int64_t total = (int64_t)tiles_m * tiles_n, blocks = (total + kXcds - 1) / kXcds * kXcds;
+    const int64_t total = (int64_t)tiles_m * tiles_n, rest = total % n_cu;
+    const int64_t n_whole = 2 * rest <= n_cu ? total - rest : total, halves = 2 * (total - n_whole);
+    auto padded = [](int64_t n) { return (n + kXcds - 1) / kXcds * kXcds; };
+    const int64_t blocks = padded(n_whole) + padded(halves);
     if (!grid_fits(blocks, 64 * kSplitWaves)) return hipErrorInvalidValue;
     const bool vec = reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0;
     static std::atomic<uint64_t> done[2];
     auto launch = [&](auto k, std::atomic<uint64_t>& d) {
         if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kRingLds, d); e != hipSuccess) return e;
-        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, vec);
+        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, (int)n_whole, vec);
         return hipGetLastError();
     };
     return bf16 ? launch(gemm_fp8_ring_kernel<true>, done[1]) : launch(gemm_fp8_ring_kernel<false>, done[0]);
@@ -467,10 +484,13 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
     const int8_t* x = static_cast<const int8_t*>(qx);
     const int8_t* w = static_cast<const int8_t*>(qw);
     const int nk = I / 128;
+    int n_cu = 0, dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n_cu < 1)
+        n_cu = 256;
     if (T <= 16) return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
     if (T <= 128) return go<2, 2, 1, 2, 4, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    if ((int64_t)T * O < 256 * 256 * 200) return go<4, 4, 2, 2, 2, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+    if ((int64_t)T * O < 256 * 256 * 100) return go<4, 4, 2, 2, 2, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+    return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, n_cu, stream);
 }
 
 }  // namespace cq
