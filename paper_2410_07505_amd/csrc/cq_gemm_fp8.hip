@@ -138,48 +138,82 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
         for (int ni = 0; ni < NT; ++ni) acc[mi][ni] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
     // weight scales of 64 steps at a time, one a lane
-    const float* ws_row = w_scale + (int64_t)((n0 + wn * 16 * NT) / 128) * nk;
-    if (n0 + wn * 16 * NT >= O) ws_row = w_scale;
+    const float* ws_row = n0 + wn * 16 * NT < O ? w_scale + (int64_t)((n0 + wn * 16 * NT) / 128) * nk : w_scale;
     float ws_all = ws_row[min(lane * WK + wk, nk - 1)];
 
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s)
+    for (int s = 0; s < S; ++s)
         if (s < steps) request(s, s);
+    if (steps >= S) __builtin_amdgcn_s_waitcnt(waitcnt_imm((S - 1) * (N + 1), 0));       // step 0 has landed
+    else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+    step_barrier();
 
     const int a_off = wk * kRows * 128 + (wm * 16 * MT + fr) * 128, b_off = wk * kRows * 128 + (TM + wn * 16 * NT + fr) * 128;
     const int sw0 = (grp ^ ((fr >> 1) & 7)) * 16, sw1 = sw0 ^ 64;
     const int s_off = P::kData + (wk * TM + wm * 16 * MT + fr) * 4;
-    auto fragment = [&](const int8_t* row) {
-        const v4i lo = *reinterpret_cast<const v4i*>(row + sw0), hi = *reinterpret_cast<const v4i*>(row + sw1);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    struct Frags {
+        v8i a[MT], b[NT];
+        float s[MT];
     };
-
-    int slot = 0;
-    for (int kt = 0; kt < steps; ++kt) {
-        // step kt has landed: of this wave's share S - 2 later steps may still be in flight, fewer at the end
-        if (S > 2 && kt + S - 2 < steps) __builtin_amdgcn_s_waitcnt(waitcnt_imm((S - 2) * (N + 1), 0));
-        else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
-        step_barrier();
-        if (kt + S - 1 < steps) request(kt + S - 1, slot == 0 ? S - 1 : slot - 1);
+    auto read = [&](Frags& f, int slot) {
         const int8_t* base = lds + slot * kSlot;
-        slot = slot + 1 == S ? 0 : slot + 1;
-        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_all), kt & 63));
-        if ((kt & 63) == 63) ws_all = ws_row[min((kt + 1 + lane) * WK + wk, nk - 1)];
-        if (WK > 1 && kt * WK + wk >= nk) continue;          // the last step has fewer than WK blocks (wave-uniform)
-        v8i b[NT];
+        auto two = [](const int8_t* lo, const int8_t* hi) {
+            return __builtin_shufflevector(*reinterpret_cast<const v4i*>(lo), *reinterpret_cast<const v4i*>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        };
 #pragma unroll
-        for (int ni = 0; ni < NT; ++ni) b[ni] = fragment(base + b_off + ni * 2048);
+        for (int ni = 0; ni < NT; ++ni) f.b[ni] = two(base + b_off + sw0 + ni * 2048, base + b_off + sw1 + ni * 2048);
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
-            const v8i a = fragment(base + a_off + mi * 2048);
-            const float s = *reinterpret_cast<const float*>(base + s_off + mi * 64) * ws;
+            f.a[mi] = two(base + a_off + sw0 + mi * 2048, base + a_off + sw1 + mi * 2048);
+            f.s[mi] = *reinterpret_cast<const float*>(base + s_off + mi * 64);
+        }
+    };
+    // Step kt: its fragments are in registers; behind the barrier its slot is free (step kt + S is requested into it) and step
+    // kt + 1 has landed (its fragments are read while kt is multiplied).  A request holds its wave for some 100 clocks: waves 0-3,
+    // one of every SIMD, make theirs before they multiply, waves 4-7 after.
+    Frags f0, f1;
+    read(f0, 0);
+    int slot = 0;
+    auto step = [&](auto full_c, int kt, Frags& cur, Frags& nxt) {       // full_c: steps kt + 1 and kt + S exist
+        constexpr bool kFull = decltype(full_c)::value;
+        __builtin_amdgcn_s_waitcnt(waitcnt_imm(kFull ? (S - 2) * (N + 1) : 0, 0));
+        step_barrier();
+        if (kFull && wave < 4) request(kt + S, slot);
+        const int next_slot = slot + 1 == S ? 0 : slot + 1;
+        if (kFull || kt + 1 < steps) read(nxt, next_slot);
+        __builtin_amdgcn_sched_barrier(0);
+        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_all), kt & 63));
+        if (WK == 1 || kt * WK + wk < nk) {                   // the last step may have fewer than WK blocks (wave-uniform)
+            v4f p[2][NT];
 #pragma unroll
-            for (int ni = 0; ni < NT; ++ni) {
-                const v4f p = product128(b[ni], a);
+            for (int mi = 0; mi <= MT; ++mi) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[mi][ni][r] = __builtin_fmaf(p[r], s, acc[mi][ni][r]);
+                for (int ni = 0; ni < NT; ++ni) {
+                    if (mi < MT) p[mi & 1][ni] = product128(cur.b[ni], cur.a[mi]);
+                    if (mi > 0) {
+                        const float s = cur.s[mi - 1] * ws;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[mi - 1][ni][r] = __builtin_fmaf(p[(mi - 1) & 1][ni][r], s, acc[mi - 1][ni][r]);
+                    }
+                }
             }
         }
+        if (kFull && wave >= 4) {
+            __builtin_amdgcn_sched_barrier(0);
+            request(kt + S, slot);
+        }
+        if ((kt & 63) == 63) ws_all = ws_row[min((kt + 1 + lane) * WK + wk, nk - 1)];
+        slot = next_slot;
+    };
+    int kt = 0;
+    for (; kt + S + 1 < steps; kt += 2) {                     // two steps a turn: the fragments' registers change places
+        step(std::true_type(), kt, f0, f1);
+        step(std::true_type(), kt + 1, f1, f0);
+    }
+    for (; kt < steps; kt += 2) {
+        if (kt + S < steps) step(std::true_type(), kt, f0, f1);
+        else step(std::false_type(), kt, f0, f1);
+        if (kt + 1 < steps) step(std::false_type(), kt + 1, f1, f0);
     }
 
     const int col0 = n0 + wn * 16 * NT + 4 * NT * grp, row0 = m0 + wm * 16 * MT + fr;
@@ -487,10 +521,40 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
     int n_cu = 0, dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n_cu < 1)
         n_cu = 256;
-    if (T <= 16) return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    if (T <= 128) return go<2, 2, 1, 2, 4, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    if ((int64_t)T * O < 256 * 256 * 100) return go<4, 4, 2, 2, 2, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-    return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, n_cu, stream);
+    // The tile: the form whose estimated time is least.  A round of `at_once` tiles takes `ns` for each 128 channels of the
+    // contraction, in whole steps, and `fixed` is a launch's and a tile's beginning and end (us, all measured on one card; us for 512 x
+    // 4096 x 4096 by form: 16 x 32 49, 32 x 32 46, 32 x 64 32, 64 x 64 23.5, 64 x 128 17.4, 128 x 128 25.0, 256 x 128 32.8; for 4096 x 4096 x
+    // 4096: 128 x 128 117, 256 x 256 66).  Small tiles have more CUs at work, large ones take in less for each product.
+    struct Form {
+        int tm, tn, wk, per_cu, ns, fixed;
+    };
+    constexpr Form kForms[] = {{16, 16, 8, 1, 117, 2300}, {16, 16, 8, 2, 205, 2300}, {16, 32, 4, 2, 180, 2300}, {32, 32, 4, 1, 172, 2200},
+                               {32, 64, 4, 1, 235, 2200}, {64, 64, 2, 1, 350, 2300}, {64, 128, 2, 1, 580, 2300}, {128, 128, 1, 1, 850, 2300}};
+    auto tiles = [&](int tm, int tn) { return (int64_t)((T + tm - 1) / tm) * ((O + tn - 1) / tn); };
+    const int64_t whole = tiles(256, 256), rest = whole % n_cu;
+    // a round of whole tiles 1950, of half tiles 1330
+    int64_t best = (whole / n_cu * 1950 + (rest == 0 ? 0 : 2 * rest <= n_cu ? 1330 : 1950)) * nk + 4000;
+    int form = -1;
+    for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
+        const Form& f = kForms[i];
+        const int64_t at_once = (int64_t)n_cu * f.per_cu, rounds = (tiles(f.tm, f.tn) + at_once - 1) / at_once;
+        const int64_t time = rounds * ((nk + f.wk - 1) / f.wk * f.wk) * f.ns + f.fixed;
+        if (time < best) {
+            best = time;
+            form = i;
+        }
+    }
+    switch (form) {
+        case 0: return go<1, 1, 1, 1, 8, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 1: return go<1, 1, 1, 1, 8, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 2: return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 3: return go<2, 1, 1, 2, 4, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 4: return go<2, 2, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 5: return go<2, 2, 2, 2, 2, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 6: return go<2, 4, 2, 2, 2, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 7: return go<4, 2, 2, 4, 1, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        default: return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, n_cu, stream);
+    }
 }
 
 }  // namespace cq
