@@ -1,17 +1,21 @@
 // Attention of a decode step over the quantized key/value cache, in one pass over the codes.
 //
 //   z_p = scale log2(e) q . k_p,  k_p = a_p (code * b);   out = sum_p 2^(z_p - m) v_p / sum_p 2^(z_p - m),  m = max z_p
-// A block takes 16 MR rows (tokens x query heads that share a key/value head) and a stretch of one sequence, its four waves every
-// fourth tile of 32 positions; each wave keeps a running maximum, sum and output of its own, which meet at the end.  When a
-// sequence is split over blocks, a second kernel joins their results.
+// A pair is a sequence, a key/value head and 16 MR rows (tokens x query heads that share the head); its unit of work is 128 positions.  All
+// units in a row, pair after pair, are cut into equal stretches, one for each block that the chip holds at once: each block adds up the lengths
+// for itself to find where its stretch starts.  A block works through the pieces of pairs in its stretch, its four waves every
+// fourth tile of 32 positions, each with a running maximum, sum and output of its own, which meet at the piece's end.  A pair that lies in one
+// stretch is done then; pieces of others go to the workspace and a second kernel joins them.
+// (64 sequences of 1024 to 8192 positions, 512 pairs: with the pairs' maximum length cut into a fixed number of blocks 175 us at best, KSTREAM so.)
 //
 // Scores: the column factors go into the query, q' = q b, and the codes into the INT8 matrix instruction as they are.  The other
 // operand is q' as 16-bit fixed-point number relative to the row's largest |q'|: two signed digits, two products, an exact 32-bit
 // sum (256 high + low: at most 256 * 127 * 32512 < 2^31), off by at most 1.6e-5 (half of 1 / 32512) of that largest.  Against codes turned into
 // binary16: no conversion of K at all, at the same matrix time.  INT4 codes enter as 16 times their value (a mask or a shift).
-// Values: weights w_p = 2^(z_p - m) a_p become binary16 relative to the largest a so far (a power of two R, 2^14 / R; the sums are
-// rescaled when R grows, as for m), which leaves 38 binades below the largest weight; codes become binary16 exactly (0x6400 | u is
-// 1024 + u).  Sums, m and the sum of 2^(z - m) are binary32.
+// Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) relative to the largest a so
+// far (a power of two R, 2^14 / R; the sums are rescaled when R grows, as for m), which leaves 38 binades below the largest weight;
+// codes become binary16 exactly (0x6400 | u is 1024 + u).  With one number a weight the result was off by sqrt(2) times what its
+// own rounding to binary16 costs; the second product is in the shadow of the loads.  Sums, m and the sum of 2^(z - m) are binary32.
 //
 // No operand passes through LDS.  The score tile is keys x rows, so that a lane holds scores of one row (lane & 15) for the positions
 // 4 (lane >> 4) + r of a subtile of 16: just the contraction elements that the product with the values wants from it, in a
@@ -43,9 +47,10 @@ struct Args {
     const int32_t *table, *lengths;
     int64_t table_width, pages;
     uint16_t* out;
-    float* partial;                                        // [pair][split][rows][dim] sums, then [pair][split][rows][2] (m, l)
-    int64_t n_partials;
-    int heads, group, S, row_tiles, splits, chunk, page_shift, max_length;
+    // pieces of pairs, two a block: [piece][rows][dim] sums, [piece][rows][2] (m, l); then for each pair its first and last block
+    float* partial;
+    int64_t n_partials, n_sequences;
+    int heads, group, S, row_tiles, n_blocks, page_shift, max_length;     // n_blocks 0: a block a pair, no pieces
     float scale;
     bool bf16;
 };
@@ -76,42 +81,105 @@ struct Bytes {
     }
 };
 
-// The element of a row of `DIM` channels that byte e of fragment f holds for lane group g
+// Which of a lane's channels (neighbours, 16 or 32 at a time, see the queries' part) byte e of fragment f holds.  8 bits: fragment f is
+// a piece of 16 bytes.  4 bits: a piece's low nibbles are its even channels, its high ones the odd; a piece makes two fragments, or one
+// where it has 8 bytes only.
 template <int DIM, int BITS>
-__device__ __forceinline__ constexpr int key_channel(int f, int e, int g) {
-    return BITS == 8 ? 64 * f + 16 * g + e : DIM == 64 ? 16 * g + 2 * (e & 7) + (e >> 3) : 128 * (f >> 1) + 32 * g + 2 * e + (f & 1);
+__device__ __forceinline__ constexpr int key_run(int f, int e) {
+    return BITS == 8 ? 16 * f + e : DIM == 64 ? 2 * (e & 7) + (e >> 3) : 32 * (f >> 1) + 2 * e + (f & 1);
 }
 
 template <int DIM, int BITS>
-struct Step {                                              // 32 positions: two subtiles of 16
-    static constexpr int kKeyPiece = BITS == 4 && DIM == 64 ? 8 : 16, kKeyPieces = DIM * BITS / 8 / 4 / kKeyPiece;
-    static constexpr int kValuePiece = DIM / 16 * BITS / 8;
-    Bytes<kKeyPiece> k[2][kKeyPieces];
-    Bytes<kValuePiece> v[2][4];
-    float ka[2][4], va[2][4];
+struct Keys {                                              // of 32 positions: two subtiles of 16
+    static constexpr int kPiece = BITS == 4 && DIM == 64 ? 8 : 16, kPieces = DIM * BITS / 8 / 4 / kPiece;
+    Bytes<kPiece> c[2][kPieces];
+    float a[2][4];
+    int64_t row[2];                                        // the subtiles' first rows
+    bool off[2];                                           // on no page
+};
+template <int DIM, int BITS>
+struct Values {
+    static constexpr int kPiece = DIM / 16 * BITS / 8;
+    Bytes<kPiece> c[2][4];
+    float a[2][4];
 };
 
+// units of a sequence of n positions, in every one of its pairs
+__device__ __forceinline__ int units_of(const Args& a, int n) { return (visible(a, n, a.S - 1) + kBlockStep - 1) / kBlockStep; }
+
+// block i's stretch of `total` units is [i q + min(i, r), ...), q = total / n, r = total % n
+__device__ __forceinline__ int64_t first_unit(int64_t total, int n, int64_t i) {
+    const int64_t q = total / n, r = total % n;
+    return i * q + min(i, r);
+}
+__device__ __forceinline__ int block_of_unit(int64_t total, int n, int64_t unit) {
+    const int64_t q = total / n, r = total % n;
+    return (int)(unit < r * (q + 1) ? unit / (q + 1) : r + (unit - r * (q + 1)) / q);
+}
+
+// a wave-uniform value in scalar registers: what comes out of LDS would make vector work of all that follows from it
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t scalar(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)scalar((int)(v >> 32)) << 32 | (uint32_t)scalar((int)v));
+}
+
+template <int DIM>
+struct Shared {
+    float o[kWaves][16][DIM + 4];                          // 16 rows 4 banks apart
+    float ml[kWaves][16][2];
+};
+
+// Units [unit0, unit0 + count) of a pair.  piece < 0: that is all of it, and the result is written; otherwise where it goes.
 template <int DIM, int BITS, int MR>
-__global__ void __launch_bounds__(64 * kWaves, 2)
-attention_kernel(Args a) {
+__device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, int64_t seq, int head, int rt, int n, int unit0, int count,
+                                                int piece) {
     constexpr int kFrags = DIM / 64, kOut = DIM / 16, kRowBytes = DIM * BITS / 8;
-    constexpr int kPitch = DIM + 4;                        // floats; 16 rows 4 banks apart
-    using StepT = Step<DIM, BITS>;
-    __shared__ __align__(16) float sh_o[kWaves][16][kPitch];
-    __shared__ float sh_ml[kWaves][16][2];
+    using KeysT = Keys<DIM, BITS>;
+    using ValuesT = Values<DIM, BITS>;
+    // the values of the next positions are requested ahead too, where there are registers for that
+    constexpr bool kValuesAhead = DIM * MR <= 128;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int fr = lane & 15, grp = lane >> 4;
-    const int split = blockIdx.x % a.splits;
-    const int64_t pair = blockIdx.x / a.splits;            // (sequence, head, row tile)
-    const int rt = (int)(pair % a.row_tiles), head = (int)(pair / a.row_tiles % a.heads);
-    const int64_t seq = pair / a.row_tiles / a.heads;
     const int rows = a.S * a.group, row0 = rt * 16 * MR, tile_rows = min(16 * MR, rows - row0);
-    const int n = a.lengths[seq];
     const int s_first = row0 / a.group, s_last = (row0 + tile_rows - 1) / a.group;
     const int see_min = visible(a, n, s_first), see_max = visible(a, n, s_last);
-    const int begin = split * a.chunk, end = min(begin + a.chunk, see_max);
-    if (begin >= see_max && a.splits > 1) return;          // (the joining kernel knows)
+    const int begin = unit0 * kBlockStep, end = min(begin + count * kBlockStep, see_max);
+
+    // ---- loads of 32 positions from `pos`.  Positions on no page read page 0 and are masked.
+    const int32_t* table = a.table + seq * a.table_width;
+    const int page_mask = (1 << a.page_shift) - 1, last_page = see_max > 0 ? (see_max - 1) >> a.page_shift : 0;
+    auto load_keys = [&](KeysT& k, int pos) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int p = pos + 16 * t;                    // wave-uniform; a subtile lies within a page
+            int page = -1;
+            if (p < see_max) page = table[min(p >> a.page_shift, last_page)];
+            k.off[t] = page < 0 || page >= a.pages;
+            k.row[t] = k.off[t] ? 0 : (((int64_t)page * a.heads + head) << a.page_shift) + (p & page_mask);
+            const uint8_t* kp = a.k_codes + k.row[t] * kRowBytes;
+#pragma unroll
+            for (int c = 0; c < KeysT::kPieces; ++c)
+                k.c[t][c].load(kp + fr * kRowBytes + c * 4 * KeysT::kPiece + grp * KeysT::kPiece);
+            const float4 f = *reinterpret_cast<const float4*>(a.k_scale + k.row[t] + 4 * grp);
+            k.a[t][0] = f.x; k.a[t][1] = f.y; k.a[t][2] = f.z; k.a[t][3] = f.w;
+        }
+    };
+    auto load_values = [&](ValuesT& v, const KeysT& k) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint8_t* vp = a.v_codes + k.row[t] * kRowBytes;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v.c[t][r].load(vp + (4 * grp + r) * kRowBytes + fr * ValuesT::kPiece);
+            const float4 f = *reinterpret_cast<const float4*>(a.v_scale + k.row[t] + 4 * grp);
+            v.a[t][0] = f.x; v.a[t][1] = f.y; v.a[t][2] = f.z; v.a[t][3] = f.w;
+        }
+    };
+    KeysT keys[2];
+    ValuesT values[2];
+    int pos = begin + wave * kTile;
+    load_keys(keys[0], pos);                               // (before the queries are worked on; past the end nothing is seen)
+    if (kValuesAhead) load_values(values[0], keys[0]);
 
     // ---- the rows' queries as two digits
     v4i q_hi[MR][kFrags], q_lo[MR][kFrags];
@@ -122,19 +190,32 @@ attention_kernel(Args a) {
         const int row = min(row0 + 16 * mr + fr, rows - 1), s = row / a.group, h = head * a.group + row % a.group;
         see[mr] = visible(a, n, s);
         const uint16_t* q = a.Q + seq * a.q_batch + s * a.q_token + h * a.q_head;
-        float x[kFrags][16], top = 0.0f, bad = 0.0f;
+        // the lane's channels are runs of kRun neighbours
+        constexpr int kRun = BITS == 4 && DIM > 64 ? 32 : 16, kRuns = DIM / 4 / kRun;
+        float x[kRuns * kRun], top = 0.0f, bad = 0.0f;
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f)
+        for (int c = 0; c < kRuns * kRun; c += 8) {
+            const int d = c / kRun * 4 * kRun + grp * kRun + c % kRun;
+            const uint4 raw = *reinterpret_cast<const uint4*>(q + d);
+            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int d = key_channel<DIM, BITS>(f, e, grp);
-                const uint32_t raw = q[d];
-                float v = a.bf16 ? __uint_as_float(raw << 16) : h2f(raw);
-                if (a.k_col) v *= a.k_col[head * DIM + d];
-                x[f][e] = v;
-                top = fmaxf(top, fabsf(v));
-                bad += v * 0.0f;                           // NaN where q is no number
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t h = e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu;
+                x[c + e] = a.bf16 ? __uint_as_float(h << 16) : h2f(h);
             }
+            if (a.k_col) {
+                const float4 lo = *reinterpret_cast<const float4*>(a.k_col + head * DIM + d);
+                const float4 hi = *reinterpret_cast<const float4*>(a.k_col + head * DIM + d + 4);
+                const float b[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[c + e] *= b[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                top = fmaxf(top, fabsf(x[c + e]));
+                bad += x[c + e] * 0.0f;                    // NaN where q is no number
+            }
+        }
         top = max_groups(top);
         bad = sum_groups(bad);
         const bool live = top >= kSmallest;                // kDigits / top stays in range
@@ -148,7 +229,8 @@ attention_kernel(Args a) {
                 uint32_t hi = 0, lo = 0;
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const int v = (int)__builtin_rintf(x[f][4 * w + b] * inv), h8 = (v + 128) >> 8;
+                    // byte e of fragment f: see key_run
+                    const int v = (int)__builtin_rintf(x[key_run<DIM, BITS>(f, 4 * w + b)] * inv), h8 = (v + 128) >> 8;
                     hi |= (uint32_t)(h8 & 255) << (8 * b);
                     lo |= (uint32_t)(v & 255) << (8 * b);
                 }
@@ -165,33 +247,8 @@ attention_kernel(Args a) {
         for (int i = 0; i < kOut; ++i) o[mr][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float R = kSmallest;                                   // the power of two above every a of V so far (from 2^-100)
 
-    // ---- loads of 32 positions from `pos`.  Positions on no page read page 0 and are masked by their scale's place in `off`.
-    const int32_t* table = a.table + seq * a.table_width;
-    const int page_mask = (1 << a.page_shift) - 1, last_page = see_max > 0 ? (see_max - 1) >> a.page_shift : 0;
-    auto load = [&](StepT& st, bool (&off)[2], int pos) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int p = pos + 16 * t;                    // wave-uniform; a subtile lies within a page
-            int page = -1;
-            if (p < see_max) page = table[min(p >> a.page_shift, last_page)];
-            off[t] = page < 0 || page >= a.pages;
-            const int64_t row = off[t] ? 0 : (((int64_t)page * a.heads + head) << a.page_shift) + (p & page_mask);
-            const uint8_t* kp = a.k_codes + row * kRowBytes;
-            const uint8_t* vp = a.v_codes + row * kRowBytes;
-#pragma unroll
-            for (int c = 0; c < StepT::kKeyPieces; ++c)
-                st.k[t][c].load(kp + fr * kRowBytes + c * 4 * StepT::kKeyPiece + grp * StepT::kKeyPiece);
-            const float4 ka = *reinterpret_cast<const float4*>(a.k_scale + row + 4 * grp);
-            st.ka[t][0] = ka.x; st.ka[t][1] = ka.y; st.ka[t][2] = ka.z; st.ka[t][3] = ka.w;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) st.v[t][r].load(vp + (4 * grp + r) * kRowBytes + fr * StepT::kValuePiece);
-            const float4 va = *reinterpret_cast<const float4*>(a.v_scale + row + 4 * grp);
-            st.va[t][0] = va.x; st.va[t][1] = va.y; st.va[t][2] = va.z; st.va[t][3] = va.w;
-        }
-    };
-
-    auto work = [&](StepT& st, const bool (&off)[2], int pos) {
-        const bool masked = pos + kTile > see_min || off[0] || off[1];       // (scalar)
+    auto work = [&](KeysT& k, ValuesT& v, int pos) {
+        const bool masked = pos + kTile > see_min || k.off[0] || k.off[1];       // (scalar)
         // keys: fragments of one position a lane
         v4i kf[2][kFrags];
 #pragma unroll
@@ -202,12 +259,12 @@ attention_kernel(Args a) {
                 for (int w = 0; w < 4; ++w) {
                     uint32_t u;
                     if constexpr (BITS == 8) {
-                        u = st.k[t][f].w[w];
+                        u = k.c[t][f].w[w];
                     } else if constexpr (DIM == 64) {
-                        const uint32_t c = st.k[t][0].w[w & 1];
+                        const uint32_t c = k.c[t][0].w[w & 1];
                         u = (w < 2 ? c << 4 : c) & 0xF0F0F0F0u;
                     } else {
-                        const uint32_t c = st.k[t][f >> 1].w[w];
+                        const uint32_t c = k.c[t][f >> 1].w[w];
                         u = (f & 1 ? c : c << 4) & 0xF0F0F0F0u;
                     }
                     kf[t][f][w] = (int)u;
@@ -218,8 +275,8 @@ attention_kernel(Args a) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see_max)) st.va[t][r] = 0.0f;
-                va_top = fmaxf(va_top, st.va[t][r]);
+                if (masked && (k.off[t] || pos + 16 * t + 4 * grp + r >= see_max)) v.a[t][r] = 0.0f;
+                va_top = fmaxf(va_top, v.a[t][r]);
             }
         va_top = max_groups(va_top);
         const float R_new = fmaxf(R, __uint_as_float((__float_as_uint(va_top) & 0x7F800000u) + 0x00800000u));
@@ -229,9 +286,9 @@ attention_kernel(Args a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) st.va[t][r] *= to_weight;
+            for (int r = 0; r < 4; ++r) v.a[t][r] *= to_weight;
 
-        v8h p[MR];
+        v8h p[MR], p_rest[MR];
 #pragma unroll
         for (int mr = 0; mr < MR; ++mr) {
             float z[2][4];
@@ -245,8 +302,8 @@ attention_kernel(Args a) {
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    z[t][r] = (float)((hi[r] << 8) + lo[r]) * (row_factor[mr] * st.ka[t][r]);
-                    if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see[mr])) z[t][r] = -INFINITY;
+                    z[t][r] = (float)((hi[r] << 8) + lo[r]) * (row_factor[mr] * k.a[t][r]);
+                    if (masked && (k.off[t] || pos + 16 * t + 4 * grp + r >= see[mr])) z[t][r] = -INFINITY;
                 }
             }
             float top = m[mr];
@@ -272,9 +329,10 @@ attention_kernel(Args a) {
                 for (int r = 0; r < 4; ++r) {
                     const float e = __builtin_amdgcn_exp2f(z[t][r] - ref);
                     l[mr] += e;
-                    float w = e * st.va[t][r];
+                    float w = e * v.a[t][r];
                     if (masked && z[t][r] == -INFINITY) w = 0.0f;      // an unseen position's scale may be anything
                     p[mr][4 * t + r] = (_Float16)w;
+                    p_rest[mr][4 * t + r] = (_Float16)(w - (float)p[mr][4 * t + r]);
                 }
         }
         // values: channel kOut fr + i of the positions, i a tile of the product
@@ -287,7 +345,7 @@ attention_kernel(Args a) {
                 for (int h = 0; h < 2; ++h) {
                     // code i of positions 2 h, 2 h + 1 as unsigned numbers in the low bytes of two halves
                     const int word = BITS == 8 ? i / 4 : i / 8, byte = BITS == 8 ? i % 4 : i % 8 / 2;
-                    uint32_t x0 = st.v[t][2 * h].w[word], x1 = st.v[t][2 * h + 1].w[word];
+                    uint32_t x0 = v.c[t][2 * h].w[word], x1 = v.c[t][2 * h + 1].w[word];
                     if (BITS == 8) {
                         x0 ^= 0x80808080u;
                         x1 ^= 0x80808080u;
@@ -301,23 +359,30 @@ attention_kernel(Args a) {
                     vf[4 * t + 2 * h + 1] = c[1];
                 }
 #pragma unroll
-            for (int mr = 0; mr < MR; ++mr) o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[mr], o[mr][i], 0, 0, 0);
+            for (int mr = 0; mr < MR; ++mr) {
+                o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[mr], o[mr][i], 0, 0, 0);
+                o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_rest[mr], o[mr][i], 0, 0, 0);
+            }
         }
     };
 
-    {
-        StepT st[2];
-        bool off[2][2];
-        int pos = begin + wave * kTile;
-        if (pos < end) load(st[0], off[0], pos);
-        while (pos < end) {
-            if (pos + kBlockStep < end) load(st[1], off[1], pos + kBlockStep);
-            work(st[0], off[0], pos);
-            pos += kBlockStep;
+    while (pos < end) {
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {             // the buffers change places
+            const int next = pos + kBlockStep;
+            if (kValuesAhead) {
+                if (next < end) {
+                    load_keys(keys[turn ^ 1], next);
+                    load_values(values[turn ^ 1], keys[turn ^ 1]);
+                }
+                work(keys[turn], values[turn], pos);
+            } else {
+                load_values(values[0], keys[turn]);
+                if (next < end) load_keys(keys[turn ^ 1], next);
+                work(keys[turn], values[0], pos);
+            }
+            pos = next;
             if (pos >= end) break;
-            if (pos + kBlockStep < end) load(st[0], off[0], pos + kBlockStep);
-            work(st[1], off[1], pos);
-            pos += kBlockStep;
         }
     }
 
@@ -325,18 +390,18 @@ attention_kernel(Args a) {
     const float unit = R / kWeightTop;
 #pragma unroll
     for (int mr = 0; mr < MR; ++mr) {
-        if (mr > 0) __syncthreads();
+        __syncthreads();                                   // (what the last piece or rows left has been read)
         const float sum = sum_groups(l[mr]);
         if (grp == 0) {
-            sh_ml[wave][fr][0] = m[mr];
-            sh_ml[wave][fr][1] = sum;
+            sh.ml[wave][fr][0] = m[mr];
+            sh.ml[wave][fr][1] = sum;
         }
         // lane: channels kOut (4 grp + r) + i of row fr
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < kOut; i += 4)
-                *reinterpret_cast<float4*>(&sh_o[wave][fr][kOut * (4 * grp + r) + i]) =
+                *reinterpret_cast<float4*>(&sh.o[wave][fr][kOut * (4 * grp + r) + i]) =
                     make_float4(o[mr][i][r] * unit, o[mr][i + 1][r] * unit, o[mr][i + 2][r] * unit, o[mr][i + 3][r] * unit);
         __syncthreads();
         constexpr int kCols = DIM / 16;                    // channels a thread joins
@@ -344,23 +409,23 @@ attention_kernel(Args a) {
         if (in_tile >= tile_rows) continue;
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh_ml[w][row][0]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
         const float ref = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, acc[kCols];
 #pragma unroll
         for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sh_ml[w][row][0] - ref);
-            total = __builtin_fmaf(f, sh_ml[w][row][1], total);
+            const float f = __builtin_amdgcn_exp2f(sh.ml[w][row][0] - ref);
+            total = __builtin_fmaf(f, sh.ml[w][row][1], total);
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) acc[c] = __builtin_fmaf(f, sh_o[w][row][d0 + c], acc[c]);
+            for (int c = 0; c < kCols; ++c) acc[c] = __builtin_fmaf(f, sh.o[w][row][d0 + c], acc[c]);
         }
         if (a.v_col) {
 #pragma unroll
             for (int c = 0; c < kCols; ++c) acc[c] *= a.v_col[head * DIM + d0 + c];
         }
-        if (a.splits == 1) {
+        if (piece < 0) {
             const int rr = row0 + in_tile, s = rr / a.group, h = head * a.group + rr % a.group;
             uint16_t* y = a.out + ((seq * a.S + s) * (int64_t)(a.heads * a.group) + h) * DIM + d0;
 #pragma unroll
@@ -369,7 +434,7 @@ attention_kernel(Args a) {
                 y[c] = a.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : (uint16_t)f2h(v);
             }
         } else {
-            const int64_t at = (pair * a.splits + split) * min(16 * MR, rows) + in_tile;
+            const int64_t at = (int64_t)piece * min(16 * MR, rows) + in_tile;
 #pragma unroll
             for (int c = 0; c < kCols; ++c) a.partial[at * DIM + d0 + c] = acc[c];
             if (d0 == 0) {
@@ -381,45 +446,150 @@ attention_kernel(Args a) {
     }
 }
 
-// One block a row: dim / 4 lanes for the channels, the others share the splits.
+template <int DIM, int BITS, int MR>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+attention_kernel(Args a) {
+    __shared__ __align__(16) Shared<DIM> sh;
+    __shared__ int64_t sh_sum[kWaves], sh_at[2];
+    const int per_seq = a.heads * a.row_tiles, tid = threadIdx.x;          // pairs of a sequence
+    int64_t total = 0, at = 0, end = 0;
+    int seq, j, unit, n, u;
+    if (a.n_blocks == 0) {
+        seq = blockIdx.x / per_seq;
+        j = blockIdx.x - seq * per_seq;
+        unit = 0;
+        n = a.lengths[seq];
+        u = units_of(a, n);
+        end = u;
+    } else {
+        // where this block's stretch starts: a thread adds up neighbouring sequences
+        const int64_t each = (a.n_sequences + 64 * kWaves - 1) / (64 * kWaves), s0 = min(tid * each, a.n_sequences), s1 = min(s0 + each, a.n_sequences);
+        int64_t mine = 0;
+        for (int64_t q = s0; q < s1; ++q) mine += units_of(a, a.lengths[q]);
+        int64_t upto = mine;                                   // inclusive sums over the wave
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t v = __shfl_up((long long)upto, d, 64);
+            if ((tid & 63) >= d) upto += v;
+        }
+        if ((tid & 63) == 63) sh_sum[tid >> 6] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < tid >> 6) upto += sh_sum[w];
+            total += sh_sum[w];
+        }
+        total = scalar(total * per_seq);
+        at = first_unit(total, a.n_blocks, blockIdx.x);
+        end = first_unit(total, a.n_blocks, blockIdx.x + 1);
+        if (at >= end) return;                                 // (block-uniform)
+        if ((upto - mine) * per_seq <= at && at < upto * per_seq) {
+            int64_t before = upto - mine;
+            for (int64_t q = s0; q < s1; ++q) {
+                const int u = units_of(a, a.lengths[q]);
+                if (at < (before + u) * per_seq) {
+                    sh_at[0] = q;
+                    sh_at[1] = before;
+                    break;
+                }
+                before += u;
+            }
+        }
+        __syncthreads();
+        seq = scalar((int)sh_at[0]);
+        n = a.lengths[seq];
+        u = units_of(a, n);
+        const int64_t in_seq = at - scalar(sh_at[1]) * per_seq;
+        j = (int)(in_seq / u);
+        unit = (int)(in_seq - (int64_t)j * u);
+    }
+    int* ends = reinterpret_cast<int*>(a.partial + a.n_partials * (DIM + 2));
+    while (true) {
+        const int count = (int)min((int64_t)(u - unit), end - at);
+        if (a.n_blocks != 0 && unit == 0 && tid == 0) {
+            const int64_t pair = (int64_t)seq * per_seq + j;
+            ends[2 * pair] = blockIdx.x;
+            ends[2 * pair + 1] = block_of_unit(total, a.n_blocks, at + u - 1);
+        }
+        // a stretch has at most one piece that continues a pair and one that only begins one
+        attention_piece<DIM, BITS, MR>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
+                                       count == u ? -1 : 2 * blockIdx.x + (unit == 0 ? 1 : 0));
+        at += count;
+        if (at >= end) break;
+        unit = 0;
+        if (++j == per_seq) {                              // a unit is left, so there is a sequence with one
+            j = 0;
+            do {
+                n = a.lengths[++seq];
+                u = units_of(a, n);
+            } while (u == 0);
+        }
+    }
+}
+
+// One block a row: dim / 4 lanes for the channels, the others share the splits, whose (m, l) the threads read side by side (one after
+// the other, 512 splits cost 100 us).
 template <int DIM>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(Args a, int rows_per_tile) {
-    constexpr int kLanesPerSplit = DIM / 4, kShares = 256 / kLanesPerSplit;
-    __shared__ float4 sh[kShares][kLanesPerSplit];
-    __shared__ float sh_l[kShares];
+    constexpr int kLanes = DIM / 4, kShares = 256 / kLanes;
+    __shared__ float4 sh[kShares][kLanes];
+    __shared__ float sh_f[256], sh_top[4], sh_l[4];
     const int rows = a.S * a.group;
     const int row = blockIdx.x % rows;
     const int64_t sh_pair = blockIdx.x / rows;             // (sequence, head)
     const int head = (int)(sh_pair % a.heads);
     const int64_t seq = sh_pair / a.heads;
     const int rt = row / rows_per_tile, in_tile = row - rt * rows_per_tile;
-    const int s_last = min((rt + 1) * rows_per_tile, rows) - 1;
-    const int see = visible(a, a.lengths[seq], s_last / a.group);
-    const int used = (see + a.chunk - 1) / a.chunk;
-    const int64_t first = (sh_pair * a.row_tiles + rt) * a.splits;
-    const int share = threadIdx.x / kLanesPerSplit, c = threadIdx.x % kLanesPerSplit;
-    const int per = min(rows_per_tile, rows);
+    const int per = min(rows_per_tile, rows), tid = threadIdx.x;
+    int first = 0, used = 0;                               // a pair without a unit has no piece, and its rows are zero
+    if (units_of(a, a.lengths[seq]) > 0) {
+        const int* ends = reinterpret_cast<const int*>(a.partial + a.n_partials * (DIM + 2)) + 2 * (sh_pair * a.row_tiles + rt);
+        first = ends[0];
+        used = ends[1] - first + 1;
+        if (used == 1) return;                             // done by its one block
+    }
+    // the pair's first block left its piece in the second of its places, the others in their first
+    auto row_of = [&](int k) { return ((int64_t)2 * (first + k) + (k == 0 ? 1 : 0)) * per + in_tile; };
     const float* ml = a.partial + a.n_partials * DIM;
     float top = -INFINITY;
-    for (int k = 0; k < used; ++k) top = fmaxf(top, ml[((first + k) * per + in_tile) * 2]);
+    for (int k = tid; k < used; k += 256) top = fmaxf(top, ml[row_of(k) * 2]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((tid & 63) == 0) sh_top[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sh_top[0], sh_top[1]), fmaxf(sh_top[2], sh_top[3]));
     const float ref = top == -INFINITY ? 0.0f : top;
+    const int share = tid / kLanes, c = tid % kLanes;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float total = 0.0f;
-    for (int k = share; k < used; k += kShares) {
-        const int64_t at = (first + k) * per + in_tile;
-        const float f = __builtin_amdgcn_exp2f(ml[at * 2] - ref);
-        const float4 v = *reinterpret_cast<const float4*>(a.partial + at * DIM + 4 * c);
-        total = __builtin_fmaf(f, ml[at * 2 + 1], total);
-        acc.x = __builtin_fmaf(f, v.x, acc.x);
-        acc.y = __builtin_fmaf(f, v.y, acc.y);
-        acc.z = __builtin_fmaf(f, v.z, acc.z);
-        acc.w = __builtin_fmaf(f, v.w, acc.w);
+    for (int k0 = 0; k0 < used; k0 += 256) {
+        const int n = min(256, used - k0);
+        __syncthreads();
+        if (tid < n) {
+            const float2 v = *reinterpret_cast<const float2*>(ml + row_of(k0 + tid) * 2);
+            const float f = __builtin_amdgcn_exp2f(v.x - ref);
+            sh_f[tid] = f;
+            total = __builtin_fmaf(f, v.y, total);
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int k = share; k < n; k += kShares) {
+            const float4 v = *reinterpret_cast<const float4*>(a.partial + row_of(k0 + k) * DIM + 4 * c);
+            const float f = sh_f[k];
+            acc.x = __builtin_fmaf(f, v.x, acc.x);
+            acc.y = __builtin_fmaf(f, v.y, acc.y);
+            acc.z = __builtin_fmaf(f, v.z, acc.z);
+            acc.w = __builtin_fmaf(f, v.w, acc.w);
+        }
     }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
+    if ((tid & 63) == 0) sh_l[tid >> 6] = total;
     sh[share][c] = acc;
-    if (c == 0) sh_l[share] = total;
     __syncthreads();
     if (share != 0) return;
+    total = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
 #pragma unroll
     for (int k = 1; k < kShares; ++k) {
         const float4 v = sh[k][c];
@@ -427,7 +597,6 @@ attention_join_kernel(Args a, int rows_per_tile) {
         acc.y += v.y;
         acc.z += v.z;
         acc.w += v.w;
-        total += sh_l[k];
     }
     const float f[4] = {acc.x, acc.y, acc.z, acc.w};
     uint16_t* y = a.out + ((seq * a.S + row / a.group) * (int64_t)(a.heads * a.group) + head * a.group + row % a.group) * DIM + 4 * c;
@@ -440,11 +609,10 @@ attention_join_kernel(Args a, int rows_per_tile) {
     *reinterpret_cast<uint2*>(y) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }
 
-// How a call is cut: 16 or 32 rows a block, and sequences into stretches of `chunk` positions so that some kBlocks blocks come
-// out (a CU holds two or three), but none of fewer than one step of its four waves.
-constexpr int kBlocks = 1024;
+// How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two a CU, three of the smallest form), or a block
+// a pair where pairs are short or so many that their lengths even out.
 struct Plan {
-    int mr, row_tiles, splits, chunk;
+    int mr, row_tiles, n_blocks;
     int64_t pairs;
 };
 Plan plan(const CacheView& c, const AttentionShape& s) {
@@ -453,20 +621,19 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.mr = rows > 16 && c.dim < 256 ? 2 : 1;
     p.row_tiles = (rows + 16 * p.mr - 1) / (16 * p.mr);
     p.pairs = s.B * c.heads * p.row_tiles;
-    const int64_t want = (kBlocks + p.pairs - 1) / p.pairs, steps = (s.max_length + kBlockStep - 1) / kBlockStep;
-    const int64_t per = (steps + std::min(want, steps) - 1) / std::min(want, steps);        // steps of a block
-    p.chunk = (int)(per * kBlockStep);
-    p.splits = (int)((steps + per - 1) / per);
+    p.n_blocks = c.dim == 64 && p.mr == 1 ? 768 : 512;
+    if (s.max_length <= kBlockStep || p.pairs >= 8 * p.n_blocks) p.n_blocks = 0;
     return p;
 }
 int64_t partials(const CacheView& c, const AttentionShape& s, const Plan& p) {
-    return p.splits > 1 ? p.pairs * p.splits * std::min(16 * p.mr, s.S * (s.q_heads / c.heads)) : 0;
+    return (int64_t)2 * p.n_blocks * std::min(16 * p.mr, s.S * (s.q_heads / c.heads));
 }
 
 }  // namespace
 
 int64_t cache_attention_workspace(const CacheView& c, const AttentionShape& s) {
-    return partials(c, s, plan(c, s)) * (c.dim + 2) * 4;
+    const Plan p = plan(c, s);
+    return p.n_blocks ? partials(c, s, p) * (c.dim + 2) * 4 + p.pairs * 8 : 0;
 }
 
 hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, const uint16_t* Q, int64_t q_batch, int64_t q_token,
@@ -474,14 +641,14 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
                                   float scale, uint16_t* out, float* workspace, hipStream_t stream) {
     const Plan p = plan(c, s);
     const int group = s.q_heads / c.heads;
-    const int64_t blocks = p.pairs * p.splits, rows = s.B * c.heads * s.S * group;
+    const int64_t blocks = p.n_blocks ? p.n_blocks : p.pairs, rows = s.B * c.heads * s.S * group;
     if (!grid_fits(blocks, 64 * kWaves) || !grid_fits(rows, 256)) return hipErrorInvalidValue;
     Args a;
     a.Q = Q; a.q_batch = q_batch; a.q_token = q_token; a.q_head = q_head;
     a.k_codes = c.k_codes; a.v_codes = c.v_codes; a.k_scale = c.k_scale; a.v_scale = c.v_scale; a.k_col = c.k_col; a.v_col = c.v_col;
     a.table = table; a.lengths = lengths; a.table_width = table_width; a.pages = c.pages;
     a.out = out; a.partial = workspace; a.n_partials = partials(c, s, p);
-    a.heads = c.heads; a.group = group; a.S = s.S; a.row_tiles = p.row_tiles; a.splits = p.splits; a.chunk = p.chunk;
+    a.heads = c.heads; a.group = group; a.S = s.S; a.row_tiles = p.row_tiles; a.n_blocks = p.n_blocks; a.n_sequences = s.B;
     a.page_shift = c.page_shift; a.max_length = s.max_length; a.scale = scale; a.bf16 = bf16;
     auto go = [&](auto kernel) { kernel<<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a); };
     if (c.bits == 8) {
@@ -493,7 +660,7 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
         else if (c.dim == 128) p.mr == 2 ? go(attention_kernel<128, 4, 2>) : go(attention_kernel<128, 4, 1>);
         else go(attention_kernel<256, 4, 1>);
     }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_blocks == 0) return e;
     auto join = [&](auto kernel) { kernel<<<(unsigned)rows, 256, 0, stream>>>(a, 16 * p.mr); };
     if (c.dim == 64) join(attention_join_kernel<64>);
     else if (c.dim == 128) join(attention_join_kernel<128>);
