@@ -1,7 +1,7 @@
 // Attention of a decode step over the quantized key/value cache, in one pass over the codes.
 //
 //   z_p = scale log2(e) q . k_p,  k_p = a_p (code * b);   out = sum_p 2^(z_p - m) v_p / sum_p 2^(z_p - m),  m = max z_p
-// A pair is a sequence, a key/value head and 16 MR rows (tokens x query heads that share the head); its unit of work is 128 positions.  All
+// A pair is a sequence, a key/value head and 16 MR rows (tokens x query heads that share the head); its unit of work is one step of a block, 128 positions.  All
 // units in a row, pair after pair, are cut into equal stretches, one for each block that the chip holds at once: each block adds up the lengths
 // for itself to find where its stretch starts.  A block works through the pieces of pairs in its stretch, its four waves every
 // fourth tile of 32 positions, each with a running maximum, sum and output of its own, which meet at the piece's end.  A pair that lies in one
@@ -20,7 +20,7 @@
 // No operand passes through LDS.  The score tile is keys x rows, so that a lane holds scores of one row (lane & 15) for the positions
 // 4 (lane >> 4) + r of a subtile of 16: just the contraction elements that the product with the values wants from it, in a
 // position order that the loads of V follow.  A lane loads V for neighbouring channels of those positions and sorts the bytes.
-// Bound by the cache's way from memory: 32 positions are requested while the 32 before are worked on.
+// Bound by the cache's way from memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -33,8 +33,8 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
-constexpr int kTile = 32;                                  // positions of a wave's step
-constexpr int kBlockStep = kWaves * kTile;
+constexpr int kSub = 2;                                    // subtiles of 16 positions that a wave works on at a time
+constexpr int kTile = 16 * kSub, kBlockStep = kWaves * kTile;
 constexpr float kDigits = 32512.0f;                        // 127 * 256
 constexpr float kWeightTop = 16384.0f;                     // 2^14
 constexpr float kSmallest = 7.888609052210118e-31f;        // 2^-100: queries and scales below count as zero
@@ -58,13 +58,19 @@ struct Args {
 // positions that token s of a sequence of n positions sees
 __device__ __forceinline__ int visible(const Args& a, int n, int s) { return min(max(n - (a.S - 1 - s), 0), a.max_length); }
 
-__device__ __forceinline__ float max_groups(float v) {     // over the four lanes that share a row
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+// over the four lanes that share a row: the swap leaves one row of 16 (half of 32) lanes twice in the first and the other twice in
+// the second register
+__device__ __forceinline__ float max_groups(float v) {
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 __device__ __forceinline__ float sum_groups(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
 // N bytes per lane, N = 2 .. 32
@@ -90,18 +96,18 @@ __device__ __forceinline__ constexpr int key_run(int f, int e) {
 }
 
 template <int DIM, int BITS>
-struct Keys {                                              // of 32 positions: two subtiles of 16
+struct Keys {                                              // of a wave's subtiles
     static constexpr int kPiece = BITS == 4 && DIM == 64 ? 8 : 16, kPieces = DIM * BITS / 8 / 4 / kPiece;
-    Bytes<kPiece> c[2][kPieces];
-    float a[2][4];
-    int64_t row[2];                                        // the subtiles' first rows
-    bool off[2];                                           // on no page
+    Bytes<kPiece> c[kSub][kPieces];
+    float a[kSub][4];
+    int64_t row[kSub];                                     // the subtiles' first rows
+    bool off[kSub];                                        // on no page
 };
 template <int DIM, int BITS>
 struct Values {
     static constexpr int kPiece = DIM / 16 * BITS / 8;
-    Bytes<kPiece> c[2][4];
-    float a[2][4];
+    Bytes<kPiece> c[kSub][4];
+    float a[kSub][4];
 };
 
 // units of a sequence of n positions, in every one of its pairs
@@ -136,8 +142,6 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     constexpr int kFrags = DIM / 64, kOut = DIM / 16, kRowBytes = DIM * BITS / 8;
     using KeysT = Keys<DIM, BITS>;
     using ValuesT = Values<DIM, BITS>;
-    // the values of the next positions are requested ahead too, where there are registers for that
-    constexpr bool kValuesAhead = DIM * MR <= 128;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int fr = lane & 15, grp = lane >> 4;
@@ -146,15 +150,22 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     const int see_min = visible(a, n, s_first), see_max = visible(a, n, s_last);
     const int begin = unit0 * kBlockStep, end = min(begin + count * kBlockStep, see_max);
 
-    // ---- loads of 32 positions from `pos`.  Positions on no page read page 0 and are masked.
+    // ---- loads of a tile's positions from `pos`.  Positions on no page read page 0 and are masked.
     const int32_t* table = a.table + seq * a.table_width;
     const int page_mask = (1 << a.page_shift) - 1, last_page = see_max > 0 ? (see_max - 1) >> a.page_shift : 0;
-    auto load_keys = [&](KeysT& k, int pos) {
+    // A tile's page numbers come from a register that holds those of the wave's next 32 tiles: asked of the table tile by tile they
+    // would stand in front of every tile's loads.
+    static_assert(kSub == 2, "two lanes a tile");
+    int pages = -1;
+    auto load_pages = [&](int pos) {                       // of the tiles at pos, pos + kBlockStep, ..
+        const int64_t p = pos + (int64_t)(lane >> 1) * kBlockStep + 16 * (lane & 1);
+        pages = p < see_max ? table[min((int)(p >> a.page_shift), last_page)] : -1;
+    };
+    auto load_keys = [&](KeysT& k, int pos, int tile) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < kSub; ++t) {
             const int p = pos + 16 * t;                    // wave-uniform; a subtile lies within a page
-            int page = -1;
-            if (p < see_max) page = table[min(p >> a.page_shift, last_page)];
+            const int page = __builtin_amdgcn_readlane(pages, (2 * tile + t) & 63);
             k.off[t] = page < 0 || page >= a.pages;
             k.row[t] = k.off[t] ? 0 : (((int64_t)page * a.heads + head) << a.page_shift) + (p & page_mask);
             const uint8_t* kp = a.k_codes + k.row[t] * kRowBytes;
@@ -167,7 +178,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     };
     auto load_values = [&](ValuesT& v, const KeysT& k) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < kSub; ++t) {
             const uint8_t* vp = a.v_codes + k.row[t] * kRowBytes;
 #pragma unroll
             for (int r = 0; r < 4; ++r) v.c[t][r].load(vp + (4 * grp + r) * kRowBytes + fr * ValuesT::kPiece);
@@ -175,11 +186,12 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
             v.a[t][0] = f.x; v.a[t][1] = f.y; v.a[t][2] = f.z; v.a[t][3] = f.w;
         }
     };
-    KeysT keys[2];
-    ValuesT values[2];
-    int pos = begin + wave * kTile;
-    load_keys(keys[0], pos);                               // (before the queries are worked on; past the end nothing is seen)
-    if (kValuesAhead) load_values(values[0], keys[0]);
+    KeysT k;
+    ValuesT v;
+    int pos = begin + wave * kTile, tile = 0;
+    load_pages(pos);
+    load_keys(k, pos, 0);                                     // (before the queries are worked on; past the end nothing is seen)
+    load_values(v, k);
 
     // ---- the rows' queries as two digits
     v4i q_hi[MR][kFrags], q_lo[MR][kFrags];
@@ -247,12 +259,20 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         for (int i = 0; i < kOut; ++i) o[mr][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float R = kSmallest;                                   // the power of two above every a of V so far (from 2^-100)
 
-    auto work = [&](KeysT& k, ValuesT& v, int pos) {
-        const bool masked = pos + kTile > see_min || k.off[0] || k.off[1];       // (scalar)
-        // keys: fragments of one position a lane
-        v4i kf[2][kFrags];
+    // Keys are requested for the next positions as soon as the scores are out, values as soon as they are summed: one set of registers
+    // each, and always something on its way.
+    while (pos < end) {
+        const int next = pos + kBlockStep;
+        bool off[kSub], masked = pos + kTile > see_min;        // (scalar)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kSub; ++t) {
+            off[t] = k.off[t];
+            masked = masked || off[t];
+        }
+        float z[MR][kSub][4];
+#pragma unroll
+        for (int t = 0; t < kSub; ++t) {
+            v4i kf[kFrags];                                // fragments of one position a lane
 #pragma unroll
             for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -267,15 +287,34 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
                         const uint32_t c = k.c[t][f >> 1].w[w];
                         u = (f & 1 ? c : c << 4) & 0xF0F0F0F0u;
                     }
-                    kf[t][f][w] = (int)u;
+                    kf[f][w] = (int)u;
                 }
-        // the scale of V's weights
+#pragma unroll
+            for (int mr = 0; mr < MR; ++mr) {
+                v4i hi = v4i{0, 0, 0, 0}, lo = v4i{0, 0, 0, 0};
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) {
+                    hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[f], q_hi[mr][f], hi, 0, 0, 0);
+                    lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[f], q_lo[mr][f], lo, 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    z[mr][t][r] = (float)((hi[r] << 8) + lo[r]) * (row_factor[mr] * k.a[t][r]);
+                    if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see[mr])) z[mr][t][r] = -INFINITY;
+                }
+            }
+        }
+        if (next < end) {
+            if ((++tile & 31) == 0) load_pages(next);
+            load_keys(k, next, tile);
+        }
+        // the scale of the weights
         float va_top = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kSub; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (masked && (k.off[t] || pos + 16 * t + 4 * grp + r >= see_max)) v.a[t][r] = 0.0f;
+                if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see_max)) v.a[t][r] = 0.0f;
                 va_top = fmaxf(va_top, v.a[t][r]);
             }
         va_top = max_groups(va_top);
@@ -284,33 +323,18 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         R = R_new;
         const float to_weight = kWeightTop / R_new;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kSub; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) v.a[t][r] *= to_weight;
 
-        v8h p[MR], p_rest[MR];
+        v8h p[MR][kSub / 2], p_rest[MR][kSub / 2];
 #pragma unroll
         for (int mr = 0; mr < MR; ++mr) {
-            float z[2][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                v4i hi = v4i{0, 0, 0, 0}, lo = v4i{0, 0, 0, 0};
-#pragma unroll
-                for (int f = 0; f < kFrags; ++f) {
-                    hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][f], q_hi[mr][f], hi, 0, 0, 0);
-                    lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][f], q_lo[mr][f], lo, 0, 0, 0);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    z[t][r] = (float)((hi[r] << 8) + lo[r]) * (row_factor[mr] * k.a[t][r]);
-                    if (masked && (k.off[t] || pos + 16 * t + 4 * grp + r >= see[mr])) z[t][r] = -INFINITY;
-                }
-            }
             float top = m[mr];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kSub; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, z[t][r]);
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, z[mr][t][r]);
             top = max_groups(top);
             const float ref = top == -INFINITY ? 0.0f : top;
             const float keep = __builtin_amdgcn_exp2f(m[mr] - ref);
@@ -324,23 +348,24 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
                     for (int r = 0; r < 4; ++r) o[mr][i][r] *= factor;
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(z[t][r] - ref);
+                    const float e = __builtin_amdgcn_exp2f(z[mr][t][r] - ref);
                     l[mr] += e;
                     float w = e * v.a[t][r];
-                    if (masked && z[t][r] == -INFINITY) w = 0.0f;      // an unseen position's scale may be anything
-                    p[mr][4 * t + r] = (_Float16)w;
-                    p_rest[mr][4 * t + r] = (_Float16)(w - (float)p[mr][4 * t + r]);
+                    if (masked && z[mr][t][r] == -INFINITY) w = 0.0f;  // an unseen position's scale may be anything
+                    const _Float16 w16 = (_Float16)w;
+                    p[mr][t / 2][4 * (t & 1) + r] = w16;
+                    p_rest[mr][t / 2][4 * (t & 1) + r] = (_Float16)(w - (float)w16);
                 }
         }
         // values: channel kOut fr + i of the positions, i a tile of the product
 #pragma unroll
         for (int i = 0; i < kOut; ++i) {
-            v8h vf;
+            v8h vf[kSub / 2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // code i of positions 2 h, 2 h + 1 as unsigned numbers in the low bytes of two halves
@@ -355,35 +380,19 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
                     }
                     const uint32_t u = __builtin_amdgcn_perm(x1, x0, 0x0C040C00u + 0x00010001u * byte) | 0x64006400u;
                     const v2h c = __builtin_bit_cast(v2h, u) - (v2h)(_Float16)(BITS == 8 ? 1152.0f : 1032.0f);
-                    vf[4 * t + 2 * h] = c[0];
-                    vf[4 * t + 2 * h + 1] = c[1];
+                    vf[t / 2][4 * (t & 1) + 2 * h] = c[0];
+                    vf[t / 2][4 * (t & 1) + 2 * h + 1] = c[1];
                 }
 #pragma unroll
-            for (int mr = 0; mr < MR; ++mr) {
-                o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[mr], o[mr][i], 0, 0, 0);
-                o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p_rest[mr], o[mr][i], 0, 0, 0);
-            }
-        }
-    };
-
-    while (pos < end) {
+            for (int mr = 0; mr < MR; ++mr)
 #pragma unroll
-        for (int turn = 0; turn < 2; ++turn) {             // the buffers change places
-            const int next = pos + kBlockStep;
-            if (kValuesAhead) {
-                if (next < end) {
-                    load_keys(keys[turn ^ 1], next);
-                    load_values(values[turn ^ 1], keys[turn ^ 1]);
+                for (int c = 0; c < kSub / 2; ++c) {
+                    o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[c], p[mr][c], o[mr][i], 0, 0, 0);
+                    o[mr][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[c], p_rest[mr][c], o[mr][i], 0, 0, 0);
                 }
-                work(keys[turn], values[turn], pos);
-            } else {
-                load_values(values[0], keys[turn]);
-                if (next < end) load_keys(keys[turn ^ 1], next);
-                work(keys[turn], values[0], pos);
-            }
-            pos = next;
-            if (pos >= end) break;
         }
+        if (next < end) load_values(v, k);
+        pos = next;
     }
 
     // ---- the waves' results meet: 16 rows at a time
@@ -447,7 +456,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
 }
 
 template <int DIM, int BITS, int MR>
-__global__ void __launch_bounds__(64 * kWaves, 2)
+__global__ void __launch_bounds__(64 * kWaves, MR == 1 ? DIM == 64 ? 4 : DIM == 128 ? 3 : 2 : 2)
 attention_kernel(Args a) {
     __shared__ __align__(16) Shared<DIM> sh;
     __shared__ int64_t sh_sum[kWaves], sh_at[2];
@@ -458,7 +467,7 @@ attention_kernel(Args a) {
         seq = blockIdx.x / per_seq;
         j = blockIdx.x - seq * per_seq;
         unit = 0;
-        n = a.lengths[seq];
+        n = scalar(a.lengths[seq]);
         u = units_of(a, n);
         end = u;
     } else {
@@ -480,8 +489,8 @@ attention_kernel(Args a) {
             total += sh_sum[w];
         }
         total = scalar(total * per_seq);
-        at = first_unit(total, a.n_blocks, blockIdx.x);
-        end = first_unit(total, a.n_blocks, blockIdx.x + 1);
+        at = scalar(first_unit(total, a.n_blocks, blockIdx.x));
+        end = scalar(first_unit(total, a.n_blocks, blockIdx.x + 1));
         if (at >= end) return;                                 // (block-uniform)
         if ((upto - mine) * per_seq <= at && at < upto * per_seq) {
             int64_t before = upto - mine;
@@ -497,11 +506,11 @@ attention_kernel(Args a) {
         }
         __syncthreads();
         seq = scalar((int)sh_at[0]);
-        n = a.lengths[seq];
+        n = scalar(a.lengths[seq]);
         u = units_of(a, n);
         const int64_t in_seq = at - scalar(sh_at[1]) * per_seq;
-        j = (int)(in_seq / u);
-        unit = (int)(in_seq - (int64_t)j * u);
+        j = scalar((int)(in_seq / u));
+        unit = scalar((int)(in_seq - (int64_t)j * u));
     }
     int* ends = reinterpret_cast<int*>(a.partial + a.n_partials * (DIM + 2));
     while (true) {
@@ -520,7 +529,7 @@ attention_kernel(Args a) {
         if (++j == per_seq) {                              // a unit is left, so there is a sequence with one
             j = 0;
             do {
-                n = a.lengths[++seq];
+                n = scalar(a.lengths[++seq]);
                 u = units_of(a, n);
             } while (u == 0);
         }
@@ -609,7 +618,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
     *reinterpret_cast<uint2*>(y) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }
 
-// How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two a CU, three of the smallest form), or a block
+// How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two to four a CU), or a block
 // a pair where pairs are short or so many that their lengths even out.
 struct Plan {
     int mr, row_tiles, n_blocks;
@@ -621,7 +630,7 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.mr = rows > 16 && c.dim < 256 ? 2 : 1;
     p.row_tiles = (rows + 16 * p.mr - 1) / (16 * p.mr);
     p.pairs = s.B * c.heads * p.row_tiles;
-    p.n_blocks = c.dim == 64 && p.mr == 1 ? 768 : 512;
+    p.n_blocks = p.mr > 1 || c.dim == 256 ? 512 : c.dim == 128 ? 768 : 1024;
     if (s.max_length <= kBlockStep || p.pairs >= 8 * p.n_blocks) p.n_blocks = 0;
     return p;
 }
