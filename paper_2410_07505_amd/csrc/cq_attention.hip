@@ -14,7 +14,7 @@
 // binary16: no conversion of K at all, at the same matrix time.  INT4 codes enter as 16 times their value (a mask or a shift).
 // Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) relative to the largest a so
 // far (a power of two R, 2^14 / R; the sums are rescaled when R grows, as for m), which leaves 38 binades below the largest weight;
-// codes become binary16 exactly (0x6400 | u is 1024 + u).  With one number a weight the result was off by sqrt(2) times what its
+// codes become binary16 exactly (as subnormal numbers, and from there in one fused step).  With one number a weight the result was off by sqrt(2) times what its
 // own rounding to binary16 costs; the second product is in the shadow of the loads.  Sums, m and the sum of 2^(z - m) are binary32.
 //
 // No operand passes through LDS.  The score tile is keys x rows, so that a lane holds scores of one row (lane & 15) for the positions
@@ -231,9 +231,12 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         top = max_groups(top);
         bad = sum_groups(bad);
         const bool live = top >= kSmallest;                // kDigits / top stays in range
-        const float inv = live ? kDigits / top : 0.0f;
-        // codes of 4 bits enter as 16 times their value
-        row_factor[mr] = (live ? top / kDigits : 0.0f) * (a.scale * 1.4426950408889634f * (BITS == 4 ? 0.0625f : 1.0f)) + bad;
+        // a score is the digits' product times a factor that is never negative (the digits take the scale's sign) nor zero (which times
+        // the -infinity of an unseen position would be no number)
+        const float inv = live ? (a.scale < 0.0f ? -kDigits : kDigits) / top : 0.0f;
+        // (codes of 4 bits enter as 16 times their value)
+        const float f = (live ? top / kDigits : 0.0f) * (fabsf(a.scale) * 1.4426950408889634f * (BITS == 4 ? 0.0625f : 1.0f));
+        row_factor[mr] = fmaxf(f, 1.1754943508222875e-38f) + bad;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -257,7 +260,9 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     for (int mr = 0; mr < MR; ++mr)
 #pragma unroll
         for (int i = 0; i < kOut; ++i) o[mr][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    float R = kSmallest;                                   // the power of two above every a of V so far (from 2^-100)
+    float R = kSmallest, to_weight = kWeightTop / kSmallest;      // the power of two above every a of V so far (from 2^-100)
+    // codes leave the subnormal numbers times 2^10 and without what was added to them: q 2^-14
+    const v2h code_unit = (v2h)(_Float16)1024.0f, code_zero = (v2h)(_Float16)(BITS == 8 ? -0.0078125f : -0.00048828125f);
 
     // Keys are requested for the next positions as soon as the scores are out, values as soon as they are summed: one set of registers
     // each, and always something on its way.
@@ -298,30 +303,44 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
                     lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[f], q_lo[mr][f], lo, 0, 0, 0);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    z[mr][t][r] = (float)((hi[r] << 8) + lo[r]) * (row_factor[mr] * k.a[t][r]);
-                    if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see[mr])) z[mr][t][r] = -INFINITY;
-                }
+                for (int r = 0; r < 4; ++r) z[mr][t][r] = (float)((hi[r] << 8) + lo[r]) * k.a[t][r];
             }
+        }
+        if (masked) {
+            asm volatile("");                              // (a branch: as selects it would cost every tile 40 instructions)
+#pragma unroll
+            for (int t = 0; t < kSub; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = pos + 16 * t + 4 * grp + r;
+                    bool any = false;
+#pragma unroll
+                    for (int mr = 0; mr < MR; ++mr) {
+                        const bool seen = !off[t] && at < see[mr];
+                        any = any || seen;
+                        if (!seen) z[mr][t][r] = -INFINITY;
+                    }
+                    if (!any) v.a[t][r] = 0.0f;            // an unseen position's scale may be anything
+                }
         }
         if (next < end) {
             if ((++tile & 31) == 0) load_pages(next);
             load_keys(k, next, tile);
         }
-        // the scale of the weights
+        // the scale of the weights: a power of two above every a so far
         float va_top = 0.0f;
 #pragma unroll
         for (int t = 0; t < kSub; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (masked && (off[t] || pos + 16 * t + 4 * grp + r >= see_max)) v.a[t][r] = 0.0f;
-                va_top = fmaxf(va_top, v.a[t][r]);
-            }
-        va_top = max_groups(va_top);
-        const float R_new = fmaxf(R, __uint_as_float((__float_as_uint(va_top) & 0x7F800000u) + 0x00800000u));
-        const float shrink = R / R_new;                    // powers of two
-        R = R_new;
-        const float to_weight = kWeightTop / R_new;
+            for (int r = 0; r < 4; ++r) va_top = fmaxf(va_top, v.a[t][r]);
+        float shrink = 1.0f;
+        if (__any(va_top >= R)) {                          // seldom after the first tile
+            va_top = max_groups(va_top);
+            const float R_new = fmaxf(R, __uint_as_float((__float_as_uint(va_top) & 0x7F800000u) + 0x00800000u));
+            shrink = R / R_new;
+            R = R_new;
+            to_weight = kWeightTop / R_new;
+        }
 #pragma unroll
         for (int t = 0; t < kSub; ++t)
 #pragma unroll
@@ -330,12 +349,12 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         v8h p[MR][kSub / 2], p_rest[MR][kSub / 2];
 #pragma unroll
         for (int mr = 0; mr < MR; ++mr) {
-            float top = m[mr];
+            float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) top = fmaxf(top, z[mr][t][r]);
-            top = max_groups(top);
+            top = fmaxf(m[mr], max_groups(top) * row_factor[mr]);
             const float ref = top == -INFINITY ? 0.0f : top;
             const float keep = __builtin_amdgcn_exp2f(m[mr] - ref);
             m[mr] = top;
@@ -350,14 +369,22 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
 #pragma unroll
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(z[mr][t][r] - ref);
-                    l[mr] += e;
-                    float w = e * v.a[t][r];
-                    if (masked && z[mr][t][r] == -INFINITY) w = 0.0f;  // an unseen position's scale may be anything
-                    const _Float16 w16 = (_Float16)w;
-                    p[mr][t / 2][4 * (t & 1) + r] = w16;
-                    p_rest[mr][t / 2][4 * (t & 1) + r] = (_Float16)(w - (float)w16);
+                for (int r = 0; r < 4; r += 2) {
+                    typedef float v2f __attribute__((ext_vector_type(2)));
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r], row_factor[mr], -ref));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r + 1], row_factor[mr], -ref));
+                    l[mr] += e0 + e1;
+                    v2f w = {e0 * v.a[t][r], e1 * v.a[t][r + 1]};
+                    // (of two rows one may see a position whose scale is no number, and the other not)
+                    if (MR > 1 && masked) w = v2f{e0 == 0.0f ? 0.0f : w[0], e1 == 0.0f ? 0.0f : w[1]};
+                    const v2h w16 = __builtin_convertvector(w, v2h);
+                    const v2f rest = {__builtin_fmaf((float)w16[0], -1.0f, w[0]), __builtin_fmaf((float)w16[1], -1.0f, w[1])};
+                    const v2h rest16 = __builtin_convertvector(rest, v2h);
+                    const int at = 4 * (t & 1) + r;
+                    p[mr][t / 2][at] = w16[0];
+                    p[mr][t / 2][at + 1] = w16[1];
+                    p_rest[mr][t / 2][at] = rest16[0];
+                    p_rest[mr][t / 2][at + 1] = rest16[1];
                 }
         }
         // values: channel kOut fr + i of the positions, i a tile of the product
@@ -368,7 +395,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    // code i of positions 2 h, 2 h + 1 as unsigned numbers in the low bytes of two halves
+                    // code i of positions 2 h, 2 h + 1 plus 128 (8) as the low bytes of two halves: subnormal numbers of 2^-24
                     const int word = BITS == 8 ? i / 4 : i / 8, byte = BITS == 8 ? i % 4 : i % 8 / 2;
                     uint32_t x0 = v.c[t][2 * h].w[word], x1 = v.c[t][2 * h + 1].w[word];
                     if (BITS == 8) {
@@ -378,8 +405,8 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
                         x0 = ((x0 ^ 0x88888888u) >> (i & 1 ? 4 : 0)) & 0x0F0F0F0Fu;
                         x1 = ((x1 ^ 0x88888888u) >> (i & 1 ? 4 : 0)) & 0x0F0F0F0Fu;
                     }
-                    const uint32_t u = __builtin_amdgcn_perm(x1, x0, 0x0C040C00u + 0x00010001u * byte) | 0x64006400u;
-                    const v2h c = __builtin_bit_cast(v2h, u) - (v2h)(_Float16)(BITS == 8 ? 1152.0f : 1032.0f);
+                    const uint32_t u = __builtin_amdgcn_perm(x1, x0, 0x0C040C00u + 0x00010001u * byte);
+                    const v2h c = __builtin_elementwise_fma(__builtin_bit_cast(v2h, u), code_unit, code_zero);
                     vf[t / 2][4 * (t & 1) + 2 * h] = c[0];
                     vf[t / 2][4 * (t & 1) + 2 * h + 1] = c[1];
                 }
@@ -396,7 +423,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     }
 
     // ---- the waves' results meet: 16 rows at a time
-    const float unit = R / kWeightTop;
+    const float unit = R;                                  // of 2^14 / R a weight and 2^-14 a code
 #pragma unroll
     for (int mr = 0; mr < MR; ++mr) {
         __syncthreads();                                   // (what the last piece or rows left has been read)
