@@ -114,7 +114,9 @@ def _check(status: int) -> None:
 _FASTCALL_PATH = os.path.join(_HERE, "_fastcall" + importlib.machinery.EXTENSION_SUFFIXES[0])
 _FAST_ENTRIES = ("crossquant_absmax", "crossquant_quantize", "crossquant_absmax_quantize", "crossquant_quantize_fp6",
                  "crossquant_absmax_batched", "crossquant_quantize_batched", "crossquant_kernel_count", "crossquant_kernel_analysis", "crossquant_w8a8_linear", "crossquant_w4a4_linear",
-                 "crossquant_fp6_packed_bytes", "crossquant_fp6_packed_weight_bytes")
+                 "crossquant_fp6_packed_bytes", "crossquant_fp6_packed_weight_bytes",
+                 "crossquant_quantize_fp8", "crossquant_weight_quantize_fp8", "crossquant_fp8_linear", "crossquant_cache_write", "crossquant_cache_read",
+                 "crossquant_cache_attention_workspace", "crossquant_cache_attention")
 _NOT_PLAIN = 1
 
 
@@ -122,6 +124,7 @@ class _NoFastcall:
     """Stands in where there is no native part for this Python and torch: nothing is plain."""
     absmax = quantize = absmax_quantize = quantize_fp6 = absmax_batched = quantize_batched = staticmethod(lambda *args: _NOT_PLAIN)
     kernel_count = kernel_analysis = w8a8_linear = w4a4_linear = absmax
+    quantize_fp8 = weight_quantize_fp8 = fp8_linear = cache_bytes = cache_write = cache_read = cache_attention = absmax
 
 
 def _load_fastcall():
@@ -782,6 +785,11 @@ def crossquant_quantize_fp8(X: torch.Tensor, *, codes: torch.Tensor = None, scal
     """e4m3 codes of X (float16 or bfloat16 [T][I]) with a scale for every 128 channels of a token.
 
     Returns (codes [T][Ip], scale float32 [Ip / 128][T]); Ip is I up to a multiple of 128, the codes past I are zero."""
+    out = _fast.quantize_fp8(X, codes, scale)
+    if out.__class__ is not int:
+        return out
+    if out != _NOT_PLAIN:
+        _check(out)
     if not isinstance(X, torch.Tensor):
         raise TypeError("X must be a torch.Tensor")
     kind = _type(X.dtype, "X")
@@ -805,6 +813,11 @@ def crossquant_weight_quantize_fp8(W: torch.Tensor, *, qw: torch.Tensor = None, 
     """e4m3 codes of a weight W (float16 or bfloat16 [I][O]) with a scale for every block of 128 x 128.
 
     Returns (qw [O][Ip], w_scale float32 [ceil(O / 128)][Ip / 128]); Ip is I up to a multiple of 128."""
+    out = _fast.weight_quantize_fp8(W, qw, w_scale)
+    if out.__class__ is not int:
+        return out
+    if out != _NOT_PLAIN:
+        _check(out)
     if not isinstance(W, torch.Tensor) or W.dim() != 2:
         raise TypeError("W must be a 2-D tensor")
     kind = _type(W.dtype, "W")
@@ -830,6 +843,11 @@ def crossquant_fp8_linear(qx: torch.Tensor, x_scale: torch.Tensor, qw: torch.Ten
     """Y = X . W on e4m3 codes with block scales.  qx [T][I], x_scale float32 [I / 128][T], qw [O][I], w_scale float32
     [ceil(O / 128)][I / 128], I a multiple of 128 (crossquant_quantize_fp8 and crossquant_weight_quantize_fp8 pad to one).
     dtype: of the result, float16 (without Y the default) or bfloat16; Y: the result's buffer, rows may be padded."""
+    out = _fast.fp8_linear(qx, x_scale, qw, w_scale, dtype, Y)
+    if out.__class__ is not int:
+        return out
+    if out != _NOT_PLAIN:
+        _check(out)
     _matrix(qx, _fp8, "qx")
     _matrix(qw, _fp8, "qw")
     if not qx.is_contiguous() or not qw.is_contiguous():
@@ -865,8 +883,17 @@ class CrossQuantCache:
     """A key/value cache of CrossQuant codes: what crossquant_cache returns and the cache calls take.  It keeps the tensors it was
     made of (k_codes, k_scale, v_codes, v_scale, k_col, v_col), which stay the caller's to read, copy or clear."""
 
-    __slots__ = ("k_codes", "k_scale", "v_codes", "v_scale", "k_col", "v_col", "bits", "alpha", "pages", "page_size", "heads", "dim",
-                 "_struct", "_address")
+    __slots__ = ("_struct", "k_codes", "k_scale", "v_codes", "v_scale", "k_col", "v_col", "bits", "alpha")
+
+    def __init__(self, struct, k_codes, k_scale, v_codes, v_scale, k_col, v_col, bits, alpha):
+        self._struct = struct                         # (bytes of a cq_cache: what the C entries read)
+        self.k_codes, self.k_scale, self.v_codes, self.v_scale = k_codes, k_scale, v_codes, v_scale
+        self.k_col, self.v_col, self.bits, self.alpha = k_col, v_col, bits, alpha
+
+    pages = property(lambda self: self.k_codes.shape[0])
+    heads = property(lambda self: self.k_codes.shape[1])
+    page_size = property(lambda self: self.k_codes.shape[2])
+    dim = property(lambda self: self.k_codes.shape[3] * 8 // self.bits)
 
 
 def crossquant_cache(k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torch.Tensor, v_scale: torch.Tensor, bits: int, *,
@@ -875,30 +902,28 @@ def crossquant_cache(k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torc
     [pages][heads][page_size][dim / 2] (bits 4); k_scale, v_scale: float32 [pages][heads][page_size]; k_col, v_col: float32
     [heads][dim], the column factors (col_scale of crossquant_quantize for calibration keys and values with the same alpha).
     A place that has not been written holds what the tensors held."""
-    if bits not in (4, 8):
-        raise CrossQuantError(-3)
-    if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
-        raise TypeError("k_codes must be a 4-D tensor")
-    pages, heads, page_size, row = k_codes.shape
-    dim = row if bits == 8 else 2 * row
-    code_type = torch.int8 if bits == 8 else torch.uint8
-    _buf(k_codes, code_type, (pages, heads, page_size, row), "k_codes", k_codes)
-    _buf(v_codes, code_type, (pages, heads, page_size, row), "v_codes", k_codes)
-    _buf(k_scale, torch.float32, (pages, heads, page_size), "k_scale", k_codes)
-    _buf(v_scale, torch.float32, (pages, heads, page_size), "v_scale", k_codes)
-    if k_col is not None:
-        _buf(k_col, torch.float32, (heads, dim), "k_col", k_codes)
-    if v_col is not None:
-        _buf(v_col, torch.float32, (heads, dim), "v_col", k_codes)
-    if not 0.0 <= alpha <= 1.0:
-        raise CrossQuantError(-4)
-    c = CrossQuantCache()
-    c.k_codes, c.k_scale, c.v_codes, c.v_scale, c.k_col, c.v_col = k_codes, k_scale, v_codes, v_scale, k_col, v_col
-    c.bits, c.alpha, c.pages, c.page_size, c.heads, c.dim = bits, float(alpha), pages, page_size, heads, dim
-    c._struct = _CacheStruct(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(k_col), _ptr(v_col),
-                             pages, page_size, heads, dim, bits, alpha)
-    c._address = ctypes.addressof(c._struct)
-    return c
+    struct = _fast.cache_bytes(k_codes, k_scale, v_codes, v_scale, bits, alpha, k_col, v_col)
+    if struct.__class__ is not bytes:
+        if bits not in (4, 8):
+            raise CrossQuantError(-3)
+        if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
+            raise TypeError("k_codes must be a 4-D tensor")
+        pages, heads, page_size, row = k_codes.shape
+        dim = row if bits == 8 else 2 * row
+        code_type = torch.int8 if bits == 8 else torch.uint8
+        _buf(k_codes, code_type, (pages, heads, page_size, row), "k_codes", k_codes)
+        _buf(v_codes, code_type, (pages, heads, page_size, row), "v_codes", k_codes)
+        _buf(k_scale, torch.float32, (pages, heads, page_size), "k_scale", k_codes)
+        _buf(v_scale, torch.float32, (pages, heads, page_size), "v_scale", k_codes)
+        if k_col is not None:
+            _buf(k_col, torch.float32, (heads, dim), "k_col", k_codes)
+        if v_col is not None:
+            _buf(v_col, torch.float32, (heads, dim), "v_col", k_codes)
+        if not 0.0 <= alpha <= 1.0:
+            raise CrossQuantError(-4)
+        struct = bytes(_CacheStruct(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(k_col), _ptr(v_col),
+                                    pages, page_size, heads, dim, bits, alpha))
+    return CrossQuantCache(struct, k_codes, k_scale, v_codes, v_scale, k_col, v_col, bits, float(alpha))
 
 
 def _cache(cache) -> torch.Tensor:
@@ -929,6 +954,12 @@ def _slots(slots, like: torch.Tensor) -> int:
 def crossquant_cache_write(cache: CrossQuantCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantizes keys and values (float16 or bfloat16 [T][heads][dim], rows may be strided) into the places slots (int32 [T]):
     place s % page_size of page s / page_size.  Slots that are negative or past the cache write nothing; a slot may occur once."""
+    if cache.__class__ is CrossQuantCache:
+        status = _fast.cache_write(cache._struct, cache.k_codes, K, V, slots)
+        if status == 0:
+            return
+        if status != _NOT_PLAIN:
+            _check(status)
     like = _cache(cache)
     T = _slots(slots, like)
     if not isinstance(K, torch.Tensor):
@@ -938,13 +969,19 @@ def crossquant_cache_write(cache: CrossQuantCache, K: torch.Tensor, V: torch.Ten
     kt, kh = _rows(K, shape, K.dtype, "K", like)
     vt, vh = _rows(V, shape, K.dtype, "V", like)
     _on_gpu(like, "the cache")
-    _launch(lib.crossquant_cache_write, like, cache._address, K.data_ptr(), kt, kh, V.data_ptr(), vt, vh, kind, slots.data_ptr(), T)
+    _launch(lib.crossquant_cache_write, like, cache._struct, K.data_ptr(), kt, kh, V.data_ptr(), vt, vh, kind, slots.data_ptr(), T)
 
 
 def crossquant_cache_read(cache: CrossQuantCache, slots: torch.Tensor, *, dtype: torch.dtype = None, K: torch.Tensor = None,
                           V: torch.Tensor = None):
     """Keys and values of the places slots (int32 [T]) as float16 (without K and V the default) or bfloat16 [T][heads][dim]; rows of slots that are
     negative or past the cache are zero.  Returns (K, V)."""
+    if cache.__class__ is CrossQuantCache:
+        out = _fast.cache_read(cache._struct, cache.k_codes, slots, torch.float16 if dtype is None and K is None and V is None else dtype, K, V)
+        if out.__class__ is not int:
+            return out
+        if out != _NOT_PLAIN:
+            _check(out)
     like = _cache(cache)
     T = _slots(slots, like)
     if dtype is None:
@@ -960,14 +997,14 @@ def crossquant_cache_read(cache: CrossQuantCache, slots: torch.Tensor, *, dtype:
     else:
         _buf(V, dtype, shape, "V", like)
     _on_gpu(like, "the cache")
-    _launch(lib.crossquant_cache_read, like, cache._address, slots.data_ptr(), T, K.data_ptr(), V.data_ptr(), kind)
+    _launch(lib.crossquant_cache_read, like, cache._struct, slots.data_ptr(), T, K.data_ptr(), V.data_ptr(), kind)
     return K, V
 
 
 def crossquant_cache_attention_workspace(cache: CrossQuantCache, B: int, S: int, q_heads: int, max_length: int) -> int:
     """Bytes of workspace that crossquant_cache_attention needs for these sizes (0: none)."""
     _cache(cache)
-    n = int(lib.crossquant_cache_attention_workspace(cache._address, B, S, q_heads, max_length))
+    n = int(lib.crossquant_cache_attention_workspace(cache._struct, B, S, q_heads, max_length))
     if n < 0:
         raise CrossQuantError(-2)
     return n
@@ -982,6 +1019,12 @@ def crossquant_cache_attention(cache: CrossQuantCache, Q: torch.Tensor, page_tab
     sequence b sees its positions below lengths[b] - (S - 1 - s); a row that sees none is zero.  scale: of the scores, 1 / sqrt(dim)
     without it; max_length: a bound on the lengths that the launch is sized for (all the table holds without it).  workspace:
     uint8, at least crossquant_cache_attention_workspace(...) bytes, for this call until it is done (one is allocated without it)."""
+    if cache.__class__ is CrossQuantCache:
+        y = _fast.cache_attention(cache._struct, cache.k_codes, Q, page_table, lengths, scale, max_length, out, workspace)
+        if y.__class__ is not int:
+            return out if out is not None else y
+        if y != _NOT_PLAIN:
+            _check(y)
     like = _cache(cache)
     if not isinstance(Q, torch.Tensor) or Q.dim() != 4:
         raise TypeError("Q must be a 4-D tensor")
@@ -1003,14 +1046,14 @@ def crossquant_cache_attention(cache: CrossQuantCache, Q: torch.Tensor, page_tab
         _buf(out, Q.dtype, (B, S, q_heads, dim), "out", like)
     _on_gpu(like, "the cache")
     if workspace is None:
-        need = int(lib.crossquant_cache_attention_workspace(cache._address, B, S, q_heads, max_length))
+        need = int(lib.crossquant_cache_attention_workspace(cache._struct, B, S, q_heads, max_length))
         if need > 0:                                  # (negative: the call below says what is wrong)
             workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
         have = max(need, 0)
     else:
         have = workspace.numel() if isinstance(workspace, torch.Tensor) else 0
         _buf(workspace, torch.uint8, (have,), "workspace", like)
-    _launch(lib.crossquant_cache_attention, like, cache._address, Q.data_ptr(), qb, qs, qh, kind, B, S, q_heads,
+    _launch(lib.crossquant_cache_attention, like, cache._struct, Q.data_ptr(), qb, qs, qh, kind, B, S, q_heads,
             page_table.data_ptr(), width, lengths.data_ptr(), max_length, dim ** -0.5 if scale is None else scale, out.data_ptr(),
             _ptr(workspace), have)
     return out

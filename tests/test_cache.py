@@ -457,6 +457,46 @@ def test_a_step_of_a_layer(cq, torch, bits):
         assert torch.equal(results[-1], step()[-1])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+def test_the_calls_without_the_native_part(cq, torch, monkeypatch, kind):
+    """The Python checks and ctypes make the same calls as the binding's native part: same outputs, new or into given buffers."""
+    from paper_2410_07505_amd import binding
+    assert binding._fast is not binding._NoFastcall
+    dtype = getattr(torch, kind)
+    g = torch.Generator().manual_seed(21)
+    X = torch.randn((33, 300), generator=g).to(dtype).cuda()
+    W = torch.randn((300, 70), generator=g).to(dtype).cuda()
+    KV = torch.randn((20, 6, 64), generator=g).to(dtype).cuda()
+    slots = torch.randperm(80, generator=g)[:20].to(torch.int32).cuda()
+    Q = queries(torch, 2, 2, 4, 64, kind)
+
+    def calls():
+        q, xs = cq.crossquant_quantize_fp8(X)
+        w, ws = cq.crossquant_weight_quantize_fp8(W)
+        cache = make_cache(torch, cq, 8, 20, 2, 16, 64, seed=22)
+        table, lens = make_table(torch, cache, [150, 31])
+        cq.crossquant_cache_write(cache, KV[:, 2:4], KV[:, 4:], slots)
+        out = [q.view(torch.uint8), xs, w.view(torch.uint8), ws, cq.crossquant_fp8_linear(q, xs, w, ws, dtype=dtype), cq.crossquant_fp8_linear(q, xs, w, ws),
+               cache.k_codes, cache.v_scale, *cq.crossquant_cache_read(cache, slots), *cq.crossquant_cache_read(cache, slots, dtype=dtype),
+               cq.crossquant_cache_attention(cache, Q, table, lens), cq.crossquant_cache_attention(cache, Q, table, lens, scale=1, max_length=140)]
+        given = [torch.zeros_like(q), torch.zeros_like(xs), torch.zeros_like(w), torch.zeros_like(ws), torch.zeros_like(out[4]), torch.zeros_like(Q)]
+        a = cq.crossquant_quantize_fp8(X, codes=given[0], scale=given[1])
+        b = cq.crossquant_weight_quantize_fp8(W, qw=given[2], w_scale=given[3])
+        c = cq.crossquant_fp8_linear(*a, *b, Y=given[4])
+        d = cq.crossquant_cache_attention(cache, Q, table, lens, out=given[5])
+        k, v = torch.zeros((20, 2, 64), dtype=dtype, device="cuda"), torch.zeros((20, 2, 64), dtype=dtype, device="cuda")
+        e = cq.crossquant_cache_read(cache, slots, K=k, V=v)
+        for x, y in zip((*a, *b, c, d, *e), (*given, k, v)):
+            assert x is y
+        return out + [t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t for t in (*given, k, v)]
+
+    native = calls()
+    monkeypatch.setattr(binding, "_fast", binding._NoFastcall)
+    for x, y in zip(native, calls()):
+        assert x.dtype == y.dtype and torch.equal(x, y)
+
+
 # ---- refusals (no GPU) -----------------------------------------------------------------------------------------------
 
 P = 0x10000
