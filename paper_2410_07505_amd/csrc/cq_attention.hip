@@ -563,33 +563,92 @@ attention_kernel(Args a) {
     }
 }
 
-// One block a row: dim / 4 lanes for the channels, the others share the splits, whose (m, l) the threads read side by side (one after
-// the other, 512 splits cost 100 us).
+// A row that has pieces in several blocks (none that lies in one is worked on again): where they are, and where it goes.
+struct JoinRow {
+    int first, used, per, in_tile;                         // blocks first .. first + used - 1; used 0: no position at all, the row is zero
+    uint16_t* out;
+    // the pair's first block left its piece in the second of its places, the others in their first
+    __device__ __forceinline__ int64_t row_of(int k) const { return ((int64_t)2 * (first + k) + (k == 0 ? 1 : 0)) * per + in_tile; }
+};
+template <int DIM>
+__device__ __forceinline__ JoinRow join_row(const Args& a, int64_t id, int rows_per_tile) {
+    JoinRow j;
+    const int rows = a.S * a.group, row = (int)(id % rows);
+    const int64_t sh_pair = id / rows, seq = sh_pair / a.heads;            // (sequence, head)
+    const int head = (int)(sh_pair - seq * a.heads), rt = row / rows_per_tile;
+    j.in_tile = row - rt * rows_per_tile;
+    j.per = min(rows_per_tile, rows);
+    j.first = j.used = 0;
+    if (units_of(a, a.lengths[seq]) > 0) {
+        const int* ends = reinterpret_cast<const int*>(a.partial + a.n_partials * (DIM + 2)) + 2 * (sh_pair * a.row_tiles + rt);
+        j.first = ends[0];
+        j.used = ends[1] - j.first + 1;
+    }
+    j.out = a.out + ((seq * a.S + row / a.group) * (int64_t)(a.heads * a.group) + head * a.group + row % a.group) * DIM;
+    return j;
+}
+__device__ __forceinline__ uint32_t rounded_pair(const Args& a, float x, float y, float total) {
+    const float u = total == 0.0f ? 0.0f : x / total, v = total == 0.0f ? 0.0f : y / total;
+    if (!a.bf16) return pack_half2(u, v);
+    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)u) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v) << 16;
+}
+
+// Many rows, few pieces each: half a wave a row.  (64 sequences of 8 heads x 8 rows, most of them whole: a block a row took 10.8 us, KJOIN so.)
+template <int DIM>
+__global__ void __launch_bounds__(256)
+attention_join_rows_kernel(Args a, int rows_per_tile, int64_t total_rows) {
+    constexpr int kEach = DIM / 32;                        // channels a lane
+    const int g = threadIdx.x & 31;
+    const int64_t id = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const JoinRow j = join_row<DIM>(a, min(id, total_rows - 1), rows_per_tile);
+    const int used = id >= total_rows || j.used == 1 ? 0 : j.used;         // (half waves differ: loops run for the longer)
+    const float* ml = a.partial + a.n_partials * DIM;
+    const int most = max(used, __shfl_xor(used, 32, 64));
+    float top = -INFINITY;
+    for (int k = g; k < used; k += 32) top = fmaxf(top, ml[j.row_of(k) * 2]);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float acc[kEach], total = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kEach; ++c) acc[c] = 0.0f;
+    for (int k0 = 0; k0 < most; k0 += 32) {
+        float f = 0.0f;
+        if (k0 + g < used) {
+            const float2 v = *reinterpret_cast<const float2*>(ml + j.row_of(k0 + g) * 2);
+            f = __builtin_amdgcn_exp2f(v.x - ref);
+            total = __builtin_fmaf(f, v.y, total);
+        }
+        for (int k = 0; k < min(32, most - k0); ++k) {
+            const float fk = __shfl(f, k, 32);
+            if (k0 + k >= used) continue;
+            const float* o = a.partial + j.row_of(k0 + k) * DIM + kEach * g;
+#pragma unroll
+            for (int c = 0; c < kEach; ++c) acc[c] = __builtin_fmaf(fk, o[c], acc[c]);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) total += __shfl_xor(total, d, 64);
+    if (id >= total_rows || j.used == 1) return;
+#pragma unroll
+    for (int c = 0; c < kEach; c += 2) *reinterpret_cast<uint32_t*>(j.out + kEach * g + c) = rounded_pair(a, acc[c], acc[c + 1], total);
+}
+
+// Few rows, perhaps of many pieces: a block a row, dim / 4 lanes for the channels, the others share the pieces, whose (m, l) the
+// threads read side by side (one after the other, 512 pieces cost 100 us).
 template <int DIM>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(Args a, int rows_per_tile) {
     constexpr int kLanes = DIM / 4, kShares = 256 / kLanes;
     __shared__ float4 sh[kShares][kLanes];
     __shared__ float sh_f[256], sh_top[4], sh_l[4];
-    const int rows = a.S * a.group;
-    const int row = blockIdx.x % rows;
-    const int64_t sh_pair = blockIdx.x / rows;             // (sequence, head)
-    const int head = (int)(sh_pair % a.heads);
-    const int64_t seq = sh_pair / a.heads;
-    const int rt = row / rows_per_tile, in_tile = row - rt * rows_per_tile;
-    const int per = min(rows_per_tile, rows), tid = threadIdx.x;
-    int first = 0, used = 0;                               // a pair without a unit has no piece, and its rows are zero
-    if (units_of(a, a.lengths[seq]) > 0) {
-        const int* ends = reinterpret_cast<const int*>(a.partial + a.n_partials * (DIM + 2)) + 2 * (sh_pair * a.row_tiles + rt);
-        first = ends[0];
-        used = ends[1] - first + 1;
-        if (used == 1) return;                             // done by its one block
-    }
-    // the pair's first block left its piece in the second of its places, the others in their first
-    auto row_of = [&](int k) { return ((int64_t)2 * (first + k) + (k == 0 ? 1 : 0)) * per + in_tile; };
+    const int tid = threadIdx.x;
+    const JoinRow j = join_row<DIM>(a, blockIdx.x, rows_per_tile);
+    const int used = j.used;
+    if (used == 1) return;
     const float* ml = a.partial + a.n_partials * DIM;
     float top = -INFINITY;
-    for (int k = tid; k < used; k += 256) top = fmaxf(top, ml[row_of(k) * 2]);
+    for (int k = tid; k < used; k += 256) top = fmaxf(top, ml[j.row_of(k) * 2]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
     if ((tid & 63) == 0) sh_top[tid >> 6] = top;
@@ -603,7 +662,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
         const int n = min(256, used - k0);
         __syncthreads();
         if (tid < n) {
-            const float2 v = *reinterpret_cast<const float2*>(ml + row_of(k0 + tid) * 2);
+            const float2 v = *reinterpret_cast<const float2*>(ml + j.row_of(k0 + tid) * 2);
             const float f = __builtin_amdgcn_exp2f(v.x - ref);
             sh_f[tid] = f;
             total = __builtin_fmaf(f, v.y, total);
@@ -611,7 +670,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
         __syncthreads();
 #pragma unroll 4
         for (int k = share; k < n; k += kShares) {
-            const float4 v = *reinterpret_cast<const float4*>(a.partial + row_of(k0 + k) * DIM + 4 * c);
+            const float4 v = *reinterpret_cast<const float4*>(a.partial + j.row_of(k0 + k) * DIM + 4 * c);
             const float f = sh_f[k];
             acc.x = __builtin_fmaf(f, v.x, acc.x);
             acc.y = __builtin_fmaf(f, v.y, acc.y);
@@ -634,15 +693,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
         acc.z += v.z;
         acc.w += v.w;
     }
-    const float f[4] = {acc.x, acc.y, acc.z, acc.w};
-    uint16_t* y = a.out + ((seq * a.S + row / a.group) * (int64_t)(a.heads * a.group) + head * a.group + row % a.group) * DIM + 4 * c;
-    uint32_t q[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float v = total == 0.0f ? 0.0f : f[i] / total;
-        q[i] = a.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : f2h(v);
-    }
-    *reinterpret_cast<uint2*>(y) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+    *reinterpret_cast<uint2*>(j.out + 4 * c) = make_uint2(rounded_pair(a, acc.x, acc.y, total), rounded_pair(a, acc.z, acc.w, total));
 }
 
 // How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two to four a CU), or a block
@@ -697,10 +748,13 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
         else go(attention_kernel<256, 4, 1>);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_blocks == 0) return e;
-    auto join = [&](auto kernel) { kernel<<<(unsigned)rows, 256, 0, stream>>>(a, 16 * p.mr); };
-    if (c.dim == 64) join(attention_join_kernel<64>);
-    else if (c.dim == 128) join(attention_join_kernel<128>);
-    else join(attention_join_kernel<256>);
+    auto join = [&](auto many, auto few) {
+        if (rows >= 1024) many<<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(a, 16 * p.mr, rows);
+        else few<<<(unsigned)rows, 256, 0, stream>>>(a, 16 * p.mr);
+    };
+    if (c.dim == 64) join(attention_join_rows_kernel<64>, attention_join_kernel<64>);
+    else if (c.dim == 128) join(attention_join_rows_kernel<128>, attention_join_kernel<128>);
+    else join(attention_join_rows_kernel<256>, attention_join_kernel<256>);
     return hipGetLastError();
 }
 
