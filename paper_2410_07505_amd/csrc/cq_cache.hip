@@ -216,7 +216,7 @@ hipError_t dispatch(const CacheView& c, bool bf16, F f) {
 
 // Rows a thread takes, and blocks for the keys of T tokens: four rows, where that leaves `least` blocks.  Four share a head's
 // factors, a wait and, in the write, one power: INT4, 2 x 8 heads of 128, 16384 tokens are written in 27.5 us and read in 14.9
-// (5.7 TB/s), with one row 31.7 and 17; with fewer blocks than that one row a thread hides more of the latency (64 tokens, written:
+// (5.7 TB/s), with one row 31.7 and 16.5; with fewer blocks than that one row a thread hides more of the latency (64 tokens, written:
 // 3.0 us with one, 5.8 with four; between 128 and 1024 blocks the two are within 3 %).
 struct Stretches {
     int rows;

@@ -3,9 +3,9 @@
 // A small layer is three calls of a few microseconds each on the GPU, and checking their tensors in Python and handing the
 // arguments through ctypes took 2 to 2.6 us a call beside the 3.4 to 4.8 of the library's own entry (a launch is 2.4).  Each
 // function here takes the tensors of one public call, all of its outputs among them, asks what binding.py asks of them, and
-// calls the C entry: 64 x 256 x 256 as three calls 20.3 -> 11.1 us, which is what their kernels take.  (The FP8 and cache calls also
-// allocate what they return: KFAST.)  Whatever is not the
-// plain case (a subclass, a wrong type or shape, another device, an output that has to be allocated) is not decided here:
+// calls the C entry: 64 x 256 x 256 as three calls 20.3 -> 11.1 us, which is what their kernels take.  The FP8 and cache calls also
+// allocate what they return: an FP8 layer of that size 17.7 -> 10.2 us, a decode step's write and attention 25 -> 15.  Whatever is
+// not the plain case (a subclass, a wrong type or shape, another device, another call's output that has to be allocated) is not decided here:
 // kNotPlain, after 0.1 us, sends the caller through the checks in binding.py, which say what is wrong or make the call.
 // Nothing is kept from one call for the next.
 #define PY_SSIZE_T_CLEAN

@@ -8,7 +8,7 @@
 //
 // A block's 8 waves are WM x WN wave tiles of 16 MT tokens x 16 NT channels times WK shares of the contraction; a step is WK
 // blocks of 128, wave share wk multiplies the wk-th.  Steps go through a ring of S slots in LDS ([wk][TM + TN rows][128
-// bytes], then [wk][TM] scales), filled by requests that bypass the registers, S - 1 steps ahead of their use.
+// bytes], then [wk][TM] scales), filled by requests that bypass the registers: step k + S is requested while step k is multiplied.
 // Within a slot 16-byte chunk c of row R sits at chunk c ^ ((R >> 1) & 7), so that the 16 rows a fragment read covers fall on
 // distinct banks.  A lane reads chunks g and g + 4 of its row (g = lane >> 4): which K positions those take inside the
 // instruction does not matter, as long as both operands are read the same way.
@@ -256,21 +256,23 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
 // Large layers: 256 x 256 tiles, one share of the contraction, held to a schedule by hand.
 //
 // A wave's 128 tokens x 64 channels are multiplied token tile by token tile.  While the four products of tile mi run, those of tile
-// mi - 1 are added to their totals (the vector unit needs half the matrix unit's time for that) and the fragment of tile mi + 1 is
-// read.  A step's one barrier stands before its last tile: by then every wave has read all it needs of this step, so its place in
-// LDS is free, and what the next step needs has to have landed.  The last tile's products cover the barrier and, weight tile by
-// weight tile as they are done with, the reads of the next step's weight fragments.
+// mi - 1 are added to their totals (the vector unit needs half the matrix unit's time for that) and the fragment of tile mi + 3 is
+// read.  A step's one barrier stands before its last three tiles: by then every wave has read all it needs of this step, so its place
+// in LDS is free, and what the next step needs has to have landed.  The last tile's products cover, weight tile by weight tile as
+// they are done with, the reads of the next step's weight fragments.
 //
-// What costs time beside the matrix unit are the requests: a CU's vector memory unit takes 16 clocks for each (1 KiB), and a wave
-// stands still while its own waits there.  So every wave makes one request a token tile, 8 a step, evenly over the step, which
-// leaves the ones made last little time to land: LDS holds nearly three steps of activations beside two of weights, and the
-// requests of the first half of a step are for the next step, those of the second half for the one after that.
+// What costs time beside the matrix unit are the requests: a wave stands still while its own wait for the CU's vector memory unit
+// (some 100 clocks each), and a SIMD's other wave has its matrix unit meanwhile.  So the two waves of a SIMD request at different
+// times: waves 0-3 the weights (two steps ahead) and the token scales behind the barrier, waves 4-7 the activations, half a step's at
+// tile 0 and half at tile 3.  LDS holds
 //   weights: two slots of 32 KiB;
-//   activations: a ring of 92 pieces of 1 KiB (8 rows), 32 a step: pieces 0 .. 27 of step k + 3 and 28 .. 31 of step k + 2 take the
-//     place of step k's.  Waves 0-3 request three of the former and one of the latter, waves 4-7 four of the former;
+//   activations: five slots of 16 KiB, half a step each: half h of step k is in slot (2 k + h) mod 5.  The second half of step k + 1
+//     and the first of step k + 2 are requested in step k, into the place that step k - 1 left and the one that was free;
 //   token scales: three slots of 1 KiB.
-// Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us, two a product 857,
-// this form KRING us.
+// Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us; two a product, by all
+// waves, 857; this form 790 to 840, 2.3 to 2.4 PFLOP/s.  With operands of zeros it takes 693: the difference is the clock under power,
+// 1.9 GHz.  Matrix instructions alone from registers reach 4.5 PFLOP/s; what remains are the instructions a wave has to issue between
+// them (reads of fragments, additions, requests).
 //
 // NT = 2 is half a tile, 256 x 128 (128 x 32 a wave, half the weight requests): outputs of less than a round of the CUs, and the last
 // round of others, are covered by such where that leaves fewer CUs idle (launch_fp8_ring).
@@ -384,7 +386,7 @@ __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const f
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
             if (mi == MT - kAhead) {
-                // all of step k + 1 has landed (its requests are older than this step's seven for k + 2), and nobody reads step k
+                // all of step k + 1 has landed (waves 4-7: all but the four latest requests, for step k + 2), and nobody reads step k
                 // any more
                 if (kMore && !front) __builtin_amdgcn_s_waitcnt(waitcnt_imm(4, 0));
                 else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
