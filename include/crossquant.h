@@ -360,6 +360,7 @@ typedef struct {
  * Quantizes keys and values K, V [T][heads][dim] (type `type`; token i's row of head h starts at i * token_stride + h * head_stride
  * elements; 16-byte aligned with strides that are multiples of 8, else CQ_ERR_ALIGN) into the places slots[i], int32 [T].
  * A slot that is negative or past the cache writes nothing (padding tokens).  No other place is touched.
+ * A row with an infinity or NaN gets a factor that is none either (alpha > 0): no value that it stands for is finite.
  * A slot may occur once in a call: of several tokens with the same slot, what the place holds afterwards is undefined.
  */
 int crossquant_cache_write(const cq_cache *cache, const void *K, int64_t k_token_stride, int64_t k_head_stride, const void *V,

@@ -530,7 +530,7 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
     struct Form {
         int tm, tn, wk, per_cu, ns, fixed;
     };
-    constexpr Form kForms[] = {{16, 16, 8, 1, 117, 2300}, {16, 16, 8, 2, 205, 2300}, {16, 32, 4, 2, 180, 2300}, {32, 32, 4, 1, 172, 2200},
+    constexpr Form kForms[] = {{16, 16, 8, 1, 117, 2300}, {16, 32, 4, 2, 180, 2300}, {32, 32, 4, 1, 172, 2200},
                                {32, 64, 4, 1, 235, 2200}, {64, 64, 2, 1, 350, 2300}, {64, 128, 2, 1, 580, 2300}, {128, 128, 1, 1, 850, 2300}};
     auto tiles = [&](int tm, int tn) { return (int64_t)((T + tm - 1) / tm) * ((O + tn - 1) / tn); };
     const int64_t whole = tiles(256, 256), rest = whole % n_cu;
@@ -548,13 +548,12 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
     }
     switch (form) {
         case 0: return go<1, 1, 1, 1, 8, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 1: return go<1, 1, 1, 1, 8, 2>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 2: return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 3: return go<2, 1, 1, 2, 4, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 4: return go<2, 2, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 5: return go<2, 2, 2, 2, 2, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 6: return go<2, 4, 2, 2, 2, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
-        case 7: return go<4, 2, 2, 4, 1, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 1: return go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 2: return go<2, 1, 1, 2, 4, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 3: return go<2, 2, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 4: return go<2, 2, 2, 2, 2, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 5: return go<2, 4, 2, 2, 2, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 6: return go<4, 2, 2, 4, 1, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
         default: return go_ring(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, n_cu, stream);
     }
 }

@@ -209,6 +209,66 @@ def test_write_of_extreme_rows(cq, torch, bits, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits,kind", [(8, "float16"), (4, "bfloat16")])
+@pytest.mark.parametrize("T,heads,dim,page", [(4101, 8, 128, 64), (2100, 33, 64, 16), (1030, 17, 256, 256), (8300, 8, 128, 1024)])
+def test_write_and_read_of_many_rows(cq, torch, T, heads, dim, page, bits, kind):
+    """Several rows a thread, with a last stretch that is not whole."""
+    test_write_and_read(cq, torch, T, heads, dim, page, 0.3, True, bits, kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 2000])
+@pytest.mark.parametrize("bits,kind", [(8, "float16"), (8, "bfloat16"), (4, "float16"), (4, "bfloat16")])
+def test_write_of_quotients_near_ties(cq, torch, bits, kind, T):
+    """Every code's quotient at a tie, and a step of the type beside it; negative, tiny and huge column factors."""
+    heads, dim, page, dtype = 33, 64, 16, getattr(torch, kind)
+    q_max = 127 if bits == 8 else 7
+    cache = make_cache(torch, cq, bits, T // page + 1, heads, page, dim, alpha=1.0, seed=3)
+    for col in (cache.k_col, cache.v_col):
+        col.fill_(1.0)
+        col[1] = 3.0
+        col[2] = 1.0 / 3.0
+        col[3, ::2] = -1.0
+        col[4] = 2.0 ** -70
+        col[5] = 2.0 ** 70
+        col[6, 1::2] = 0.0
+        col[7] = 2.0 ** -149
+    g = torch.Generator().manual_seed(T + bits)
+    half = torch.randint(-q_max, q_max, (T, heads, dim), generator=g).double() + 0.5
+    X = (half * torch.tensor([1.0, 3.0, 1.0 / 3.0]).double().repeat(heads // 3)[:, None]).to(dtype)
+    away = torch.randint(-1, 2, X.shape, generator=g).to(torch.int16)
+    X = (X.view(torch.int16) + away).view(dtype)
+    X[:, :, 7] = q_max                                         # the maximum of most rows: a = 1
+    Xg = X.cuda()
+    slots = torch.randperm(cache.pages * page, generator=g)[:T].to(torch.int32)
+    cq.crossquant_cache_write(cache, Xg, Xg, slots.cuda())
+    for n in "kv":
+        q, a = row_codes(torch, X, cache.k_col.cpu(), 1.0, bits)
+        codes, scale, _ = places(torch, cache, n)
+        assert torch.equal(scale[slots.long()].cpu(), a.double()) and torch.equal(codes[slots.long()].cpu(), q)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("T", [4, 2000])
+def test_a_row_with_no_number_stands_for_none(cq, torch, T, value):
+    heads, dim, page = 33, 64, 16
+    cache = make_cache(torch, cq, 8, T // page + 1, heads, page, dim, alpha=0.3, seed=4)
+    cache.k_col[2, 9] = 0.0
+    X = torch.randn((T, heads, dim), generator=torch.Generator().manual_seed(6)).half()
+    plain = X.clone()
+    X[T // 2, 2, 11] = value
+    slots = torch.arange(T, dtype=torch.int32).cuda()
+    cq.crossquant_cache_write(cache, plain.cuda(), plain.cuda(), slots)
+    want = [t.clone() for t in cq.crossquant_cache_read(cache, slots)]
+    cq.crossquant_cache_write(cache, X.cuda(), X.cuda(), slots)
+    for w, t in zip(want, cq.crossquant_cache_read(cache, slots)):
+        assert not torch.isfinite(t[T // 2, 2]).any()
+        t[T // 2, 2] = w[T // 2, 2]
+        assert torch.equal(t, w)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [8, 4])
 def test_places_behind_four_gib(cq, torch, bits):
     """Codes and the elements behind them past 32-bit offsets: the last pages of a cache of over 2^32 bytes a side."""
@@ -272,6 +332,66 @@ def test_attention(cq, torch, case, bits, kind):
         for s in range(S):
             if n - (S - 1 - s) <= 0:
                 assert (out[b, s] == 0).all()
+
+
+# many sequences: (B, longest, S, heads, group, dim, page, bits, kind)
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,longest,S,heads,group,dim,page,bits,kind", [
+    (300, 500, 1, 2, 2, 64, 16, 8, "float16"),                 # more sequences than threads of a block
+    (130, 2500, 1, 2, 5, 128, 64, 4, "bfloat16"),              # over 1000 rows, of several pieces
+    (90, 1500, 1, 2, 7, 256, 32, 8, "bfloat16"),
+    (70, 1200, 2, 2, 9, 64, 64, 4, "float16"),                 # the same, 18 rows a pair
+    (900, 200, 1, 7, 1, 128, 16, 8, "float16"),                # a block a pair
+    (600, 160, 1, 7, 1, 256, 32, 4, "float16"),
+    (520, 300, 2, 4, 10, 64, 16, 8, "bfloat16"),
+])
+def test_attention_of_many_sequences(cq, torch, B, longest, S, heads, group, dim, page, bits, kind):
+    print("attention of %d sequences up to %d, %d x %d heads of %d" % (B, longest, heads, group, dim), flush=True)
+    g = torch.Generator().manual_seed(B)
+    lengths = torch.randint(0, longest + 1, (B,), generator=g).tolist()
+    lengths[0], lengths[B // 2], lengths[-1] = longest, 0, longest
+    cache = make_cache(torch, cq, bits, sum(-(-n // page) for n in lengths) + 1, heads, page, dim, seed=B)
+    table, lens = make_table(torch, cache, lengths, seed=B)
+    Q = queries(torch, B, S, heads * group, dim, kind, B) / float(cache.k_col.mean())
+    out = check_attention(torch, cq, cache, Q, table, lens, max_length=longest)
+    assert torch.equal(out, cq.crossquant_cache_attention(cache, Q, table, lens, max_length=longest))
+
+
+@pytest.mark.gpu
+def test_two_graphs_and_eager_calls_of_attention_at_once(cq, torch):
+    """Two graphs of one cache, each with its own workspace, on streams of their own beside eager calls; lengths and table change
+    between replays."""
+    lengths = [3000, 700, 1]
+    cache = make_cache(torch, cq, 4, 3 * 220, 2, 16, 128, seed=21)
+    table, lens = make_table(torch, cache, [3200, 900, 100], seed=5)
+    lens.copy_(torch.tensor(lengths))
+    Qs = [queries(torch, 3, s, 8, 128, "float16", s) for s in (1, 2)]
+    need = [cq.crossquant_cache_attention_workspace(cache, 3, s, 8, 3200) for s in (1, 2)]
+    streams, graphs, outs, works = [torch.cuda.Stream() for _ in range(2)], [], [], []
+    for Q, n, stream in zip(Qs, need, streams):
+        out, work = torch.empty_like(Q), torch.empty(n, dtype=torch.uint8, device="cuda")
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            cq.crossquant_cache_attention(cache, Q, table, lens, max_length=3200, out=out, workspace=work)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            cq.crossquant_cache_attention(cache, Q, table, lens, max_length=3200, out=out, workspace=work)
+        graphs.append(graph), outs.append(out), works.append(work)
+    for turn in range(4):
+        lens.add_(torch.tensor([40, 1, 7], dtype=torch.int32, device="cuda"))
+        table[0, 5 + turn] = -1
+        for out in outs:
+            out.fill_(9.0)
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        eager = [cq.crossquant_cache_attention(cache, Q, table, lens, max_length=3200) for Q in Qs]
+        torch.cuda.synchronize()
+        for out, e in zip(outs, eager):
+            assert torch.equal(out, e)
+    check_attention(torch, cq, cache, Qs[1], table, lens, max_length=3200)
 
 
 @pytest.mark.gpu

@@ -203,6 +203,18 @@ def test_linear(cq, torch, T, I, O, kind):
     assert torch.equal(Y.view(torch.int16), again.view(torch.int16))
 
 
+# one for each way to tile a layer that the shapes above leave out: tiles of 16 x 32, 32 x 64 and 64 x 128 in less than a round and with
+# ragged ends; 256 x 256 ones of one, two and three blocks of the contraction, with whole tiles alone (number no multiple of 8), with
+# halves alone, and with both
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,I,O,kind", [(1, 384, 8200, "float16"), (5, 512, 11000, "bfloat16"), (17, 384, 8200, "bfloat16"),
+                                        (64, 512, 4100, "float16"), (100, 256, 8200, "float16"), (300, 384, 4100, "bfloat16"),
+                                        (2000, 128, 11000, "float16"), (1500, 256, 8200, "bfloat16"), (700, 384, 11000, "float16"),
+                                        (1000, 1024, 4100, "bfloat16"), (2000, 384, 4100, "float16")])
+def test_linear_by_other_tiles(cq, torch, T, I, O, kind):
+    test_linear(cq, torch, T, I, O, kind)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("offset,pitch", [(0, 336), (0, 300), (4, 304), (1, 301), (2, 310)])
 @pytest.mark.parametrize("T", [5, 70, 260])
