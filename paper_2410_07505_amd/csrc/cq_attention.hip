@@ -114,14 +114,29 @@ struct Values {
 // units of a sequence of n positions, in every one of its pairs
 __device__ __forceinline__ int units_of(const Args& a, int n) { return (visible(a, n, a.S - 1) + kBlockStep - 1) / kBlockStep; }
 
-// block i's stretch of `total` units is [i q + min(i, r), ...), q = total / n, r = total % n
-__device__ __forceinline__ int64_t first_unit(int64_t total, int n, int64_t i) {
-    const int64_t q = total / n, r = total % n;
-    return i * q + min(i, r);
-}
-__device__ __forceinline__ int block_of_unit(int64_t total, int n, int64_t unit) {
-    const int64_t q = total / n, r = total % n;
-    return (int)(unit < r * (q + 1) ? unit / (q + 1) : r + (unit - r * (q + 1)) / q);
+// x / n for x >= 0, n > 0 (a division of 64 bits takes several times as long)
+__device__ __forceinline__ int64_t divide(int64_t x, int n) { return x >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)n) : x / n; }
+
+// `total` units cut for n blocks: block i's stretch is [i q + min(i, r), ...), q = total / n, r = total % n
+struct Cut {
+    int64_t q, r;
+    __device__ __forceinline__ Cut(int64_t total, int n) : q(divide(total, n)), r(total - q * n) {}
+    __device__ __forceinline__ int64_t first(int64_t i) const { return i * q + min(i, r); }
+    __device__ __forceinline__ int block_of(int64_t unit) const {
+        const int64_t longer = r * (q + 1);                // units in the stretches of q + 1
+        return (int)(unit < longer ? divide(unit, (int)q + 1) : r + divide(unit - longer, (int)q));
+    }
+};
+
+// inclusive sums over the wave's lanes
+__device__ __forceinline__ int prefix_sum(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);        // from the lanes 1, 2, 4, 8 before in a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);        // the row before's last lane, to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);        // lane 31, to rows 2 and 3
+    return v;
 }
 
 // a wave-uniform value in scalar registers: what comes out of LDS would make vector work of all that follows from it
@@ -498,8 +513,22 @@ attention_kernel(Args a) {
         n = scalar(a.lengths[seq]);
         u = units_of(a, n);
         end = u;
+    } else if (a.n_sequences <= 64) {
+        // where this block's stretch starts: each wave for itself, a lane a sequence (at most 2^24 units each)
+        const int q = tid & 63, n_q = q < a.n_sequences ? a.lengths[q] : 0, u_q = q < a.n_sequences ? units_of(a, n_q) : 0, upto = prefix_sum(u_q);
+        total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * per_seq;
+        const Cut cut(total, a.n_blocks);
+        at = cut.first(blockIdx.x);
+        end = cut.first(blockIdx.x + 1);
+        if (at >= end) return;
+        seq = __builtin_ctzll(__ballot((int64_t)upto * per_seq > at));
+        n = __builtin_amdgcn_readlane(n_q, seq);
+        u = __builtin_amdgcn_readlane(u_q, seq);
+        const int64_t in_seq = at - (int64_t)(__builtin_amdgcn_readlane(upto, seq) - u) * per_seq;
+        j = (int)divide(in_seq, u);
+        unit = (int)(in_seq - (int64_t)j * u);
     } else {
-        // where this block's stretch starts: a thread adds up neighbouring sequences
+        // the same for more: a thread adds up neighbouring sequences
         const int64_t each = (a.n_sequences + 64 * kWaves - 1) / (64 * kWaves), s0 = min(tid * each, a.n_sequences), s1 = min(s0 + each, a.n_sequences);
         int64_t mine = 0;
         for (int64_t q = s0; q < s1; ++q) mine += units_of(a, a.lengths[q]);
@@ -517,8 +546,9 @@ attention_kernel(Args a) {
             total += sh_sum[w];
         }
         total = scalar(total * per_seq);
-        at = scalar(first_unit(total, a.n_blocks, blockIdx.x));
-        end = scalar(first_unit(total, a.n_blocks, blockIdx.x + 1));
+        const Cut cut(total, a.n_blocks);
+        at = scalar(cut.first(blockIdx.x));
+        end = scalar(cut.first(blockIdx.x + 1));
         if (at >= end) return;                                 // (block-uniform)
         if ((upto - mine) * per_seq <= at && at < upto * per_seq) {
             int64_t before = upto - mine;
@@ -537,7 +567,7 @@ attention_kernel(Args a) {
         n = scalar(a.lengths[seq]);
         u = units_of(a, n);
         const int64_t in_seq = at - scalar(sh_at[1]) * per_seq;
-        j = scalar((int)(in_seq / u));
+        j = scalar((int)divide(in_seq, u));
         unit = scalar((int)(in_seq - (int64_t)j * u));
     }
     int* ends = reinterpret_cast<int*>(a.partial + a.n_partials * (DIM + 2));
@@ -546,7 +576,7 @@ attention_kernel(Args a) {
         if (a.n_blocks != 0 && unit == 0 && tid == 0) {
             const int64_t pair = (int64_t)seq * per_seq + j;
             ends[2 * pair] = blockIdx.x;
-            ends[2 * pair + 1] = block_of_unit(total, a.n_blocks, at + u - 1);
+            ends[2 * pair + 1] = count == u ? blockIdx.x : Cut(total, a.n_blocks).block_of(at + u - 1);
         }
         // a stretch has at most one piece that continues a pair and one that only begins one
         attention_piece<DIM, BITS, MR>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
@@ -648,6 +678,9 @@ attention_join_kernel(Args a, int rows_per_tile) {
     const int used = j.used;
     if (used == 1) return;
     const float* ml = a.partial + a.n_partials * DIM;
+    const int share = tid / kLanes, c = tid % kLanes;
+    float4 first = make_float4(0.0f, 0.0f, 0.0f, 0.0f);      // (asked for before its factor is known)
+    if (share < used) first = *reinterpret_cast<const float4*>(a.partial + j.row_of(share) * DIM + 4 * c);
     float top = -INFINITY;
     for (int k = tid; k < used; k += 256) top = fmaxf(top, ml[j.row_of(k) * 2]);
 #pragma unroll
@@ -656,7 +689,6 @@ attention_join_kernel(Args a, int rows_per_tile) {
     __syncthreads();
     top = fmaxf(fmaxf(sh_top[0], sh_top[1]), fmaxf(sh_top[2], sh_top[3]));
     const float ref = top == -INFINITY ? 0.0f : top;
-    const int share = tid / kLanes, c = tid % kLanes;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float total = 0.0f;
     for (int k0 = 0; k0 < used; k0 += 256) {
@@ -671,7 +703,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
         __syncthreads();
 #pragma unroll 4
         for (int k = share; k < n; k += kShares) {
-            const float4 v = *reinterpret_cast<const float4*>(a.partial + j.row_of(k0 + k) * DIM + 4 * c);
+            const float4 v = k0 + k == share ? first : *reinterpret_cast<const float4*>(a.partial + j.row_of(k0 + k) * DIM + 4 * c);
             const float f = sh_f[k];
             acc.x = __builtin_fmaf(f, v.x, acc.x);
             acc.y = __builtin_fmaf(f, v.y, acc.y);
@@ -697,8 +729,14 @@ attention_join_kernel(Args a, int rows_per_tile) {
     *reinterpret_cast<uint2*>(j.out + 4 * c) = make_uint2(rounded_pair(a, acc.x, acc.y, total), rounded_pair(a, acc.z, acc.w, total));
 }
 
-// How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two to four a CU), or a block
-// a pair where pairs are short or so many that their lengths even out.
+// How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two to four a CU), or a block a pair, which
+// needs no second kernel, where
+// - pairs have four units at most: a unit that follows another takes some 1 us, the second kernel and finding the stretches 4.  One
+//   sequence of 256 (500) positions 8.4 (10.5) us so, 11.6 (11.7) in stretches; 640 positions 11.4 and 11.8; 40 sequences of up to 500,
+//   320 pairs, 15.4 and 21.7;
+// - or they are so many that the longest one could be is no more than each of the chip's places gets of them: 1024 sequences of up to
+//   1024 positions, 8192 pairs, 289 us so and 328 in stretches; of 4096 positions, INT4, 578 and 607, but one such sequence among
+//   short ones would keep the others waiting.
 struct Plan {
     int mr, row_tiles, n_blocks;
     int64_t pairs;
@@ -710,7 +748,8 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.row_tiles = (rows + 16 * p.mr - 1) / (16 * p.mr);
     p.pairs = s.B * c.heads * p.row_tiles;
     p.n_blocks = p.mr > 1 || c.dim == 256 ? 512 : c.dim == 128 ? 768 : 1024;
-    if (s.max_length <= kBlockStep || p.pairs >= 8 * p.n_blocks) p.n_blocks = 0;
+    const int64_t longest = (s.max_length + (int64_t)kBlockStep - 1) / kBlockStep;
+    if (longest <= 4 || p.pairs >= p.n_blocks * std::max<int64_t>(8, longest)) p.n_blocks = 0;
     return p;
 }
 int64_t partials(const CacheView& c, const AttentionShape& s, const Plan& p) {

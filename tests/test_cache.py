@@ -490,15 +490,15 @@ def test_attention_with_strided_queries_and_buffers_given(cq, torch):
     table, lens = make_table(torch, cache, [500, 33])
     wide = queries(torch, 2, 3, 2 * 8 + 4, 128, "bfloat16")
     Q = wide[:, :2, 2:18]
-    need = cq.crossquant_cache_attention_workspace(cache, 2, 2, 16, 500)
+    need = cq.crossquant_cache_attention_workspace(cache, 2, 2, 16, 544)
     assert need > 0
     out = torch.full((2, 2, 16, 128), 7.0, dtype=torch.bfloat16, device="cuda")
     work = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")   # NaN patterns: need not be cleared
-    got = check_attention(torch, cq, cache, Q, table, lens, max_length=500, out=out, workspace=work[:need])
+    got = check_attention(torch, cq, cache, Q, table, lens, max_length=544, out=out, workspace=work[:need])
     assert got is out and (work[need:] == 0xFF).all()
-    assert torch.equal(out, cq.crossquant_cache_attention(cache, Q.contiguous(), table, lens, max_length=500))
+    assert torch.equal(out, cq.crossquant_cache_attention(cache, Q.contiguous(), table, lens, max_length=544))
     with pytest.raises(cq.CrossQuantError) as e:
-        cq.crossquant_cache_attention(cache, Q, table, lens, max_length=500, workspace=work[:need - 16])
+        cq.crossquant_cache_attention(cache, Q, table, lens, max_length=544, workspace=work[:need - 16])
     assert e.value.status == -2
 
 
