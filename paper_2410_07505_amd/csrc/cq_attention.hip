@@ -730,13 +730,14 @@ attention_join_kernel(Args a, int rows_per_tile) {
 }
 
 // How a call is cut: 16 or 32 rows a block; as many blocks as the chip holds at once (two to four a CU), or a block a pair, which
-// needs no second kernel, where
-// - pairs have four units at most: a unit that follows another takes some 1 us, the second kernel and finding the stretches 4.  One
-//   sequence of 256 (500) positions 8.4 (10.5) us so, 11.6 (11.7) in stretches; 640 positions 11.4 and 11.8; 40 sequences of up to 500,
-//   320 pairs, 15.4 and 21.7;
-// - or they are so many that the longest one could be is no more than each of the chip's places gets of them: 1024 sequences of up to
-//   1024 positions, 8192 pairs, 289 us so and 328 in stretches; of 4096 positions, INT4, 578 and 607, but one such sequence among
-//   short ones would keep the others waiting.
+// needs no second kernel.  A unit that follows another in a block takes some 1 us, the second kernel and finding the stretches 4, so
+// a block a pair is for pairs of at most
+// - four units: one sequence (8 pairs) of 256 (500) positions 8.4 (10.5) us so, 11.6 (11.7) in stretches, 640 positions 11.4 and 11.8;
+// - eight where they keep half the CUs busy: of up to 1024 positions, 16 sequences 17.0 and 18.8, 100 31 and 40, 200 67 and 77;
+// - sixteen where they fill the chip: of up to 2048 positions, 100 sequences 62 and 68, 400 211 and 224;
+// - what each of the chip's places gets of them where that is more still.
+// Lengths are known on the GPU only: longer ones could keep all others waiting (1024 sequences of 4096 positions, INT4, of about one
+// length: 578 and 607).
 struct Plan {
     int mr, row_tiles, n_blocks;
     int64_t pairs;
@@ -749,7 +750,7 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.pairs = s.B * c.heads * p.row_tiles;
     p.n_blocks = p.mr > 1 || c.dim == 256 ? 512 : c.dim == 128 ? 768 : 1024;
     const int64_t longest = (s.max_length + (int64_t)kBlockStep - 1) / kBlockStep;
-    if (longest <= 4 || p.pairs >= p.n_blocks * std::max<int64_t>(8, longest)) p.n_blocks = 0;
+    if (longest <= (p.pairs < 128 ? 4 : p.pairs < p.n_blocks ? 8 : std::max<int64_t>(16, p.pairs / p.n_blocks))) p.n_blocks = 0;
     return p;
 }
 int64_t partials(const CacheView& c, const AttentionShape& s, const Plan& p) {

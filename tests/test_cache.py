@@ -337,7 +337,11 @@ def test_attention(cq, torch, case, bits, kind):
 # many sequences: (B, longest, S, heads, group, dim, page, bits, kind)
 @pytest.mark.gpu
 @pytest.mark.parametrize("B,longest,S,heads,group,dim,page,bits,kind", [
-    (300, 500, 1, 2, 2, 64, 16, 8, "float16"),                 # more sequences than threads of a block
+    (300, 500, 1, 2, 2, 64, 16, 8, "float16"),
+    (300, 1500, 1, 1, 2, 64, 16, 8, "float16"),                # more sequences than threads of a block, in pieces
+    (270, 1300, 1, 1, 1, 256, 64, 4, "bfloat16"),
+    (64, 1100, 1, 1, 3, 128, 16, 8, "float16"),                # as many as a wave's lanes, and one more
+    (65, 1100, 1, 1, 3, 128, 16, 4, "float16"),
     (130, 2500, 1, 2, 5, 128, 64, 4, "bfloat16"),              # over 1000 rows, of several pieces
     (90, 1500, 1, 2, 7, 256, 32, 8, "bfloat16"),
     (70, 1200, 2, 2, 9, 64, 64, 4, "float16"),                 # the same, 18 rows a pair
