@@ -56,8 +56,8 @@ struct Args {
     bool bf16;
 };
 
-// positions that token s of a sequence of n positions sees
-__device__ __forceinline__ int visible(const Args& a, int n, int s) { return min(max(n - (a.S - 1 - s), 0), a.max_length); }
+// positions that token s of a sequence of n positions sees (n from memory: anything)
+__device__ __forceinline__ int visible(const Args& a, int n, int s) { return min(max(max(n, 0) - (a.S - 1 - s), 0), a.max_length); }
 
 // over the four lanes that share a row: the swap leaves one row of 16 (half of 32) lanes twice in the first and the other twice in
 // the second register

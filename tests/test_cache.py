@@ -399,6 +399,18 @@ def test_two_graphs_and_eager_calls_of_attention_at_once(cq, torch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("longest", [100, 2000])
+def test_attention_of_lengths_that_are_none(cq, torch, longest):
+    """Negative lengths, the smallest among them, count as zero; neighbours are not touched by them."""
+    cache = make_cache(torch, cq, 8, 300, 2, 16, 64, seed=22)
+    table, lens = make_table(torch, cache, [longest, 50, 50, 50, longest], seed=22)
+    lens[1:4] = torch.tensor([-2 ** 31, -1, -2 ** 31 + 2], dtype=torch.int32)
+    Q = queries(torch, 5, 3, 4, 64, "float16")
+    out = check_attention(torch, cq, cache, Q, table, lens)
+    assert (out[1:4] == 0).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
 def test_attention_scales(cq, torch, scale):
     """A flat, an inverted and a peaked softmax (scores of hundreds)."""
@@ -745,3 +757,9 @@ def test_calls_check_what_they_are_given(cq, torch):
         cq.crossquant_cache_attention(cache, Q, table, lens)
     with pytest.raises(TypeError, match="crossquant_cache"):
         cq.crossquant_cache_read(None, slots)
+
+
+def test_the_longest_max_length(cq):
+    c = descriptor(cq)
+    assert cq.raw.crossquant_cache_attention_workspace(c, 1, 1, 2, (1 << 31) - 256) > 0
+    assert cq.raw.crossquant_cache_attention_workspace(c, 1, 1, 2, (1 << 31) - 255) == -1
