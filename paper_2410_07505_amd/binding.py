@@ -977,7 +977,7 @@ def crossquant_cache_read(cache: CrossQuantCache, slots: torch.Tensor, *, dtype:
     """Keys and values of the places slots (int32 [T]) as float16 (without K and V the default) or bfloat16 [T][heads][dim]; rows of slots that are
     negative or past the cache are zero.  Returns (K, V)."""
     if cache.__class__ is CrossQuantCache:
-        out = _fast.cache_read(cache._struct, cache.k_codes, slots, torch.float16 if dtype is None and K is None and V is None else dtype, K, V)
+        out = _fast.cache_read(cache._struct, cache.k_codes, slots, dtype, K, V)
         if out.__class__ is not int:
             return out
         if out != _NOT_PLAIN:

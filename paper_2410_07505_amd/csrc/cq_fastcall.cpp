@@ -571,8 +571,16 @@ PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* t;
         const int32_t* slots;
         int64_t T;
-        at::ScalarType scalar;
-        if (!cache_of(a[0], a[1], c, t) || !slots_of(a[2], t->get_device(), slots, T) || !dtype(a[3], scalar) || type_of(scalar) < 0) return kNotPlain;
+        at::ScalarType scalar = at::kHalf;
+        if (!cache_of(a[0], a[1], c, t) || !slots_of(a[2], t->get_device(), slots, T)) return kNotPlain;
+        if (a[3] != Py_None) {
+            if (!dtype(a[3], scalar)) return kNotPlain;
+        } else if (a[4] != Py_None || a[5] != Py_None) {
+            const at::Tensor* given;
+            if (!tensor(a[a[4] != Py_None ? 4 : 5], given)) return kNotPlain;
+            scalar = given->scalar_type();
+        }
+        if (type_of(scalar) < 0) return kNotPlain;
         for (int i = 0; i < 2; ++i)
             if (!given_or_new(a[4 + i], out[i], {T, c->heads, c->dim}, scalar, *t)) return kNotPlain;
         void *k = out[0].data_ptr(), *v = out[1].data_ptr(), *s = c10::hip::getCurrentHIPStream(t->get_device()).stream();
