@@ -609,12 +609,11 @@ __device__ __forceinline__ JoinRow join_row(const Args& a, int64_t id, int rows_
     const int head = (int)(sh_pair - seq * a.heads), rt = row / rows_per_tile;
     j.in_tile = row - rt * rows_per_tile;
     j.per = min(rows_per_tile, rows);
-    j.first = j.used = 0;
-    if (units_of(a, a.lengths[seq]) > 0) {
-        const int* ends = reinterpret_cast<const int*>(a.partial + a.n_partials * (DIM + 2)) + 2 * (sh_pair * a.row_tiles + rt);
-        j.first = ends[0];
-        j.used = ends[1] - j.first + 1;
-    }
+    const int* ends = reinterpret_cast<const int*>(a.partial + a.n_partials * (DIM + 2)) + 2 * (sh_pair * a.row_tiles + rt);
+    const int first = ends[0], last = ends[1];             // (asked for before the length says whether they mean anything)
+    const bool any = units_of(a, a.lengths[seq]) > 0;
+    j.first = any ? first : 0;
+    j.used = any ? last - first + 1 : 0;
     j.out = a.out + ((seq * a.S + row / a.group) * (int64_t)(a.heads * a.group) + head * a.group + row % a.group) * DIM;
     return j;
 }
@@ -635,8 +634,10 @@ attention_join_rows_kernel(Args a, int rows_per_tile, int64_t total_rows) {
     const int used = id >= total_rows || j.used == 1 ? 0 : j.used;         // (half waves differ: loops run for the longer)
     const float* ml = a.partial + a.n_partials * DIM;
     const int most = max(used, __shfl_xor(used, 32, 64));
-    float top = -INFINITY;
-    for (int k = g; k < used; k += 32) top = fmaxf(top, ml[j.row_of(k) * 2]);
+    auto load = [&](int k) { return k < used ? *reinterpret_cast<const float2*>(ml + j.row_of(k) * 2) : make_float2(-INFINITY, 0.0f); };
+    const float2 first = load(g);                          // (m, l) of the first 32 pieces
+    float top = first.x;
+    for (int k = 32 + g; k < used; k += 32) top = fmaxf(top, load(k).x);
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float ref = top == -INFINITY ? 0.0f : top;
@@ -644,18 +645,23 @@ attention_join_rows_kernel(Args a, int rows_per_tile, int64_t total_rows) {
 #pragma unroll
     for (int c = 0; c < kEach; ++c) acc[c] = 0.0f;
     for (int k0 = 0; k0 < most; k0 += 32) {
-        float f = 0.0f;
-        if (k0 + g < used) {
-            const float2 v = *reinterpret_cast<const float2*>(ml + j.row_of(k0 + g) * 2);
-            f = __builtin_amdgcn_exp2f(v.x - ref);
-            total = __builtin_fmaf(f, v.y, total);
-        }
-        for (int k = 0; k < min(32, most - k0); ++k) {
-            const float fk = __shfl(f, k, 32);
-            if (k0 + k >= used) continue;
-            const float* o = a.partial + j.row_of(k0 + k) * DIM + kEach * g;
+        const float2 v = k0 == 0 ? first : load(k0 + g);
+        const float f = __builtin_amdgcn_exp2f(v.x - ref);
+        total = __builtin_fmaf(f, v.y, total);
+        for (int k = 0; k < min(32, most - k0); k += 2) {   // two pieces at a time; past the last one that one again, not used
+            float o[2][kEach];
 #pragma unroll
-            for (int c = 0; c < kEach; ++c) acc[c] = __builtin_fmaf(fk, o[c], acc[c]);
+            for (int i = 0; i < 2; ++i) {
+                const float* at = a.partial + j.row_of(max(min(k0 + k + i, used - 1), 0)) * DIM + kEach * g;
+                __builtin_memcpy(o[i], at, sizeof(o[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float fk = __shfl(f, k + i, 32);
+                if (k0 + k + i >= used) continue;
+#pragma unroll
+                for (int c = 0; c < kEach; ++c) acc[c] = __builtin_fmaf(fk, o[i][c], acc[c]);
+            }
         }
     }
 #pragma unroll
