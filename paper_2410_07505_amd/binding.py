@@ -881,14 +881,19 @@ def crossquant_fp8_linear(qx: torch.Tensor, x_scale: torch.Tensor, qw: torch.Ten
 
 class CrossQuantCache:
     """A key/value cache of CrossQuant codes: what crossquant_cache returns and the cache calls take.  It keeps the tensors it was
-    made of (k_codes, k_scale, v_codes, v_scale, k_col, v_col), which stay the caller's to read, copy or clear."""
+    made of (k_codes, k_scale, v_codes, v_scale, k_col, v_col), which stay the caller's to read, copy or clear, but not to resize:
+    the calls use the memory they had.  Its attributes cannot be replaced; another cache is another crossquant_cache."""
 
     __slots__ = ("_struct", "k_codes", "k_scale", "v_codes", "v_scale", "k_col", "v_col", "bits", "alpha")
 
-    def __init__(self, struct, k_codes, k_scale, v_codes, v_scale, k_col, v_col, bits, alpha):
-        self._struct = struct                         # (bytes of a cq_cache: what the C entries read)
-        self.k_codes, self.k_scale, self.v_codes, self.v_scale = k_codes, k_scale, v_codes, v_scale
-        self.k_col, self.v_col, self.bits, self.alpha = k_col, v_col, bits, alpha
+    def __init__(self, *values):                      # (_struct: bytes of a cq_cache, what the C entries read)
+        for name, value in zip(self.__slots__, values):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value=None):
+        raise AttributeError("a cache's %s cannot be replaced" % name)
+
+    __delattr__ = __setattr__
 
     pages = property(lambda self: self.k_codes.shape[0])
     heads = property(lambda self: self.k_codes.shape[1])
@@ -909,6 +914,8 @@ def crossquant_cache(k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torc
         if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
             raise TypeError("k_codes must be a 4-D tensor")
         pages, heads, page_size, row = k_codes.shape
+        if k_codes.numel() == 0:
+            raise CrossQuantError(-2)
         dim = row if bits == 8 else 2 * row
         code_type = torch.int8 if bits == 8 else torch.uint8
         _buf(k_codes, code_type, (pages, heads, page_size, row), "k_codes", k_codes)

@@ -494,7 +494,7 @@ PyObject* cache_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int64_t bits;
         for (int i = 0; i < 4; ++i)
             if (!tensor(a[i], t[i]) || !t[i]->is_cuda() || !t[i]->is_contiguous() || t[i]->get_device() != t[0]->get_device()) return kNotPlain;
-        if (!integer(a[4], bits) || (bits != 8 && bits != 4) || !PyFloat_CheckExact(a[5]) || t[0]->dim() != 4) return kNotPlain;
+        if (!integer(a[4], bits) || (bits != 8 && bits != 4) || !PyFloat_CheckExact(a[5]) || t[0]->dim() != 4 || t[0]->numel() == 0) return kNotPlain;
         const at::IntArrayRef shape = t[0]->sizes();
         const at::ScalarType codes = bits == 8 ? at::kChar : at::kByte;
         if (t[0]->scalar_type() != codes || t[2]->scalar_type() != codes || t[2]->sizes() != shape || t[1]->scalar_type() != at::kFloat ||

@@ -399,6 +399,20 @@ def test_two_graphs_and_eager_calls_of_attention_at_once(cq, torch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("S,group,dim,bits,kind", [(70, 3, 128, 8, "float16"), (33, 5, 64, 4, "bfloat16"), (40, 2, 256, 4, "float16"), (300, 1, 64, 8, "bfloat16")])
+def test_attention_of_a_chunk(cq, torch, S, group, dim, bits, kind):
+    """Many tokens at once, most of them in row tiles that see only a part of the sequence, or nothing of it."""
+    lengths = [S, S + 1500, 10, 0, S + 129]
+    cache = make_cache(torch, cq, bits, sum(-(-n // 32) for n in lengths), 2, 32, dim, seed=S)
+    table, lens = make_table(torch, cache, lengths, seed=S)
+    Q = queries(torch, 5, 1, 2 * group, dim, kind, S).expand(5, S, 2 * group, dim) / float(cache.k_col.mean())
+    check_attention(torch, cq, cache, Q, table, lens)
+    one = queries(torch, 1, 1, 2 * group, dim, kind, S + 1)
+    assert torch.equal(cq.crossquant_cache_attention(cache, one.expand(5, S, -1, -1), table, lens),
+                       cq.crossquant_cache_attention(cache, one.expand(5, S, -1, -1).contiguous(), table, lens))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("longest", [100, 2000])
 def test_attention_of_lengths_that_are_none(cq, torch, longest):
     """Negative lengths, the smallest among them, count as zero; neighbours are not touched by them."""
@@ -763,3 +777,31 @@ def test_the_longest_max_length(cq):
     c = descriptor(cq)
     assert cq.raw.crossquant_cache_attention_workspace(c, 1, 1, 2, (1 << 31) - 256) > 0
     assert cq.raw.crossquant_cache_attention_workspace(c, 1, 1, 2, (1 << 31) - 255) == -1
+
+
+def test_a_cache_with_an_empty_axis_is_refused(cq, torch):
+    for shape in ((0, 2, 16, 64), (4, 0, 16, 64), (4, 2, 0, 64), (4, 2, 16, 0)):
+        codes, scale = torch.zeros(shape, dtype=torch.int8), torch.zeros(shape[:3])
+        with pytest.raises(cq.CrossQuantError) as e:
+            cq.crossquant_cache(codes, scale, codes, scale, 8)
+        assert e.value.status == -2
+
+
+def test_a_cache_keeps_its_tensors(cq, torch):
+    codes, scale = torch.zeros((4, 2, 16, 64), dtype=torch.int8), torch.zeros((4, 2, 16))
+    cache = cq.crossquant_cache(codes, scale, codes, scale, 8)
+    for name in ("k_codes", "v_scale", "k_col", "alpha", "_struct", "other"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, codes)
+        with pytest.raises(AttributeError):
+            delattr(cache, name)
+    assert cache.k_codes is codes and (cache.pages, cache.heads, cache.page_size, cache.dim) == (4, 2, 16, 64)
+
+
+@pytest.mark.gpu
+def test_a_cache_with_an_empty_axis_is_refused_on_the_gpu(cq, torch):
+    for shape in ((0, 2, 16, 64), (4, 0, 16, 64)):
+        codes, scale = torch.zeros(shape, dtype=torch.int8, device="cuda"), torch.zeros(shape[:3], device="cuda")
+        with pytest.raises(cq.CrossQuantError) as e:
+            cq.crossquant_cache(codes, scale, codes, scale, 8)
+        assert e.value.status == -2
