@@ -69,6 +69,22 @@ __device__ __forceinline__ void store4(uint16_t* __restrict__ row, int col, int 
     }
 }
 
+// eight, packed, to a 16-byte aligned place
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store8(uint16_t* __restrict__ row, int col, int O, const v4u& p) {
+    if (col + 8 <= O) {
+        *reinterpret_cast<v4u*>(row + col) = p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (col + e < O) row[col + e] = (uint16_t)(e & 1 ? p[e / 2] >> 16 : p[e / 2]);
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ v4u pack8(const v4f& a, const v4f& b) {
+    return v4u{pack_pair<BF16>(a[0], a[1]), pack_pair<BF16>(a[2], a[3]), pack_pair<BF16>(b[0], b[1]), pack_pair<BF16>(b[2], b[3])};
+}
+
 template <int MT, int NT, int WM, int WN, int WK, int S>
 struct Fp8Tile {
     static_assert(WM * WN * WK == kSplitWaves, "8 waves");
@@ -283,7 +299,7 @@ static_assert(kRingLds <= 160 * 1024, "LDS of a CU");
 template <int NT, bool BF16>
 __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const float* __restrict__ x_scale,
                                           const int8_t* __restrict__ qw, const float* __restrict__ w_scale, int T, int nk, int O,
-                                          uint16_t* __restrict__ Y, int64_t ldy, bool vec, int8_t* lds, int m0, int n0) {
+                                          uint16_t* __restrict__ Y, int64_t ldy, bool vec, bool vec8, int8_t* lds, int m0, int n0) {
     constexpr int MT = 8, WN = 4, WTN = 16 * NT, kMidAt = 0, kLateAt = 3, kEarlyAt = 1, kAhead = 3;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -445,13 +461,31 @@ __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const f
         for (int r = 0; r < 4; ++r) acc[MT - 1][ni][r] = __builtin_fmaf(p[ni][r], s_old, acc[MT - 1][ni][r]);
 
     const int col0 = n0 + wn * WTN + 4 * NT * grp, row0 = m0 + wm * 128 + fr;
+    // Outputs leave 16 bytes a lane, and whole lines of 128 bytes an instruction: of its 32 bytes of a token (NT = 4) a lane keeps one
+    // half and trades the other for the same half of its neighbour's token.  (4096 x 4096 x 4096: 8 bytes a lane 63.4 us, 16 of its own token 59.1, KLINES so)
+    const int odd = lane & 1;
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
         const int row = row0 + 16 * mi;
-        if (row >= T) continue;
-        uint16_t* y = Y + (int64_t)row * ldy;
+        if (!vec8) {
+            if (row >= T) continue;
 #pragma unroll
-        for (int ni = 0; ni < NT; ++ni) store4<BF16>(y, col0 + 4 * ni, O, acc[mi][ni], vec);
+            for (int ni = 0; ni < NT; ++ni) store4<BF16>(Y + (int64_t)row * ldy, col0 + 4 * ni, O, acc[mi][ni], vec);
+        } else if (NT == 2) {
+            if (row < T) store8(Y + (int64_t)row * ldy, col0, O, pack8<BF16>(acc[mi][0], acc[mi][1]));
+        } else {
+            const v4u lo = pack8<BF16>(acc[mi][0], acc[mi][1]), hi = pack8<BF16>(acc[mi][NT - 2], acc[mi][NT - 1]);
+            v4u even, next;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(odd ? lo[i] : hi[i]), 0xB1, 0xF, 0xF, true);     // lane ^ 1
+                even[i] = odd ? other : lo[i];
+                next[i] = odd ? hi[i] : other;
+            }
+            uint16_t* y = Y + (int64_t)(row - odd) * ldy;
+            if (row - odd < T) store8(y, col0 + 8 * odd, O, even);
+            if (row - odd + 1 < T) store8(y + ldy, col0 + 8 * odd, O, next);
+        }
     }
 }
 
@@ -460,7 +494,7 @@ template <bool BF16>
 __global__ void __launch_bounds__(64 * kSplitWaves, 2)
 gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
                      const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
-                     int tiles_n, int n_whole, bool vec) {
+                     int tiles_n, int n_whole, bool vec, bool vec8) {
     extern __shared__ __align__(16) int8_t lds[];
     const int whole_blocks = (n_whole + kXcds - 1) / kXcds * kXcds;
     const bool whole = (int)blockIdx.x < whole_blocks;
@@ -471,8 +505,8 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     tile_of_index(whole ? at : n_whole + at / 2, tiles_m, tiles_n, tile_m, tile_n);
     const int m0 = tile_m * kRingTile, n0 = tile_n * kRingTile + (whole ? 0 : at % 2 * (kRingTile / 2));
     if (n0 >= O) return;                                      // the right half of a last tile may have no channel
-    if (whole) ring_tile<4, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, lds, m0, n0);
-    else ring_tile<2, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, lds, m0, n0);
+    if (whole) ring_tile<4, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, vec8, lds, m0, n0);
+    else ring_tile<2, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, vec8, lds, m0, n0);
 }
 
 hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const float* ws, int T, int nk, int O, uint16_t* Y, bool bf16,
@@ -484,10 +518,11 @@ hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const fl
     const int64_t blocks = padded(n_whole) + padded(halves);
     if (!grid_fits(blocks, 64 * kSplitWaves)) return hipErrorInvalidValue;
     const bool vec = reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0;
+    const bool vec8 = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0;
     static std::atomic<uint64_t> done[2];
     auto launch = [&](auto k, std::atomic<uint64_t>& d) {
         if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kRingLds, d); e != hipSuccess) return e;
-        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, (int)n_whole, vec);
+        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, (int)n_whole, vec, vec8);
         return hipGetLastError();
     };
     return bf16 ? launch(gemm_fp8_ring_kernel<true>, done[1]) : launch(gemm_fp8_ring_kernel<false>, done[0]);
