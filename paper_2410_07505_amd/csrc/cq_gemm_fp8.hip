@@ -55,31 +55,24 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// four neighbouring outputs of a token, those past O left out
-template <bool BF16>
-__device__ __forceinline__ void store4(uint16_t* __restrict__ row, int col, int O, const v4f& y, bool vec) {
-    const uint2 p = make_uint2(pack_pair<BF16>(y[0], y[1]), pack_pair<BF16>(y[2], y[3]));
-    if (vec && col + 4 <= O) {
-        *reinterpret_cast<uint2*>(row + col) = p;
-    } else {
-        if (col < O) row[col] = (uint16_t)p.x;
-        if (col + 1 < O) row[col + 1] = (uint16_t)(p.x >> 16);
-        if (col + 2 < O) row[col + 2] = (uint16_t)p.y;
-        if (col + 3 < O) row[col + 3] = (uint16_t)(p.y >> 16);
-    }
-}
-
-// eight, packed, to a 16-byte aligned place
+// 4 or 8 neighbouring outputs of a token as one store, wherever they lie (2-byte aligned: what a row of an odd pitch is); those past O
+// are left out.  (509 x 2816 x 4090, rows of 8180 bytes: 2 bytes at a time 19.1 us, so 13.5; 2000 x 2816 x
+// 4091 42 and 30)
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void store8(uint16_t* __restrict__ row, int col, int O, const v4u& p) {
-    if (col + 8 <= O) {
-        *reinterpret_cast<v4u*>(row + col) = p;
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+template <typename P>
+__device__ __forceinline__ void store_row(uint16_t* __restrict__ row, int col, int O, const P& p) {
+    constexpr int kCount = sizeof(P) / 2;
+    if (col + kCount <= O) {
+        __builtin_memcpy(row + col, &p, sizeof(P));
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < kCount; ++e)
             if (col + e < O) row[col + e] = (uint16_t)(e & 1 ? p[e / 2] >> 16 : p[e / 2]);
     }
 }
+template <bool BF16>
+__device__ __forceinline__ v2u pack4(const v4f& y) { return v2u{pack_pair<BF16>(y[0], y[1]), pack_pair<BF16>(y[2], y[3])}; }
 template <bool BF16>
 __device__ __forceinline__ v4u pack8(const v4f& a, const v4f& b) {
     return v4u{pack_pair<BF16>(a[0], a[1]), pack_pair<BF16>(a[2], a[3]), pack_pair<BF16>(b[0], b[1]), pack_pair<BF16>(b[2], b[3])};
@@ -103,7 +96,7 @@ template <int MT, int NT, int WM, int WN, int WK, int S, bool BF16>
 __global__ void __launch_bounds__(64 * kSplitWaves)
 gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
                 const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
-                int tiles_n, bool vec) {
+                int tiles_n) {
     using P = Fp8Tile<MT, NT, WM, WN, WK, S>;
     constexpr int TM = P::TM, kRows = P::kRows, kSlot = P::kSlot, N = P::N;
     extern __shared__ __align__(16) int8_t lds[];
@@ -232,40 +225,53 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
         if (kt + 1 < steps) step(std::false_type(), kt + 1, f1, f0);
     }
 
+    // Outputs are stored G neighbouring weight tiles at a time, 8 or 16 bytes a lane.
+    constexpr int G = NT % 2 == 0 && MT * NT / 2 >= WK ? 2 : 1, kGroups = MT * NT / G;
     const int col0 = n0 + wn * 16 * NT + 4 * NT * grp, row0 = m0 + wm * 16 * MT + fr;
+    auto store = [&](int first, const v4f* y) {               // tiles first .. first + G - 1 of mi NT + ni
+        const int row = row0 + 16 * (first / NT), col = col0 + 4 * (first % NT);
+        if (row >= T) return;
+        uint16_t* at = Y + (int64_t)row * ldy;
+        if (G == 2) store_row(at, col, O, pack8<BF16>(y[0], y[G - 1]));
+        else store_row(at, col, O, pack4<BF16>(y[0]));
+    };
     if (WK == 1) {
 #pragma unroll
-        for (int mi = 0; mi < MT; ++mi) {
-            const int row = row0 + 16 * mi;
-            if (row >= T) continue;
-            uint16_t* y = Y + (int64_t)row * ldy;
+        for (int g = 0; g < kGroups; ++g) {
+            v4f y[G];
 #pragma unroll
-            for (int ni = 0; ni < NT; ++ni) store4<BF16>(y, col0 + 4 * ni, O, acc[mi][ni], vec);
+            for (int i = 0; i < G; ++i) y[i] = acc[(g * G + i) / NT][(g * G + i) % NT];
+            store(g * G, y);
         }
         return;
     }
-    // The WK shares of a wave tile meet in LDS: tile (mi, ni) is summed and stored by share (mi NT + ni) % WK, the others hand
-    // theirs over; always summed in the order of the shares.
+    // The WK shares of a wave tile meet in LDS: group g of its tiles is summed and stored by share g % WK, the others hand theirs over;
+    // always summed in the order of the shares.
     __syncthreads();                                         // the last step's reads are done
     v4f* parts = reinterpret_cast<v4f*>(lds) + w * (MT * NT * (WK - 1) * 64) + lane;
 #pragma unroll
     for (int u = 0; u < MT * NT; ++u) {
-        const int owner = u % WK;
+        const int owner = u / G % WK;
         if (wk != owner) parts[(u * (WK - 1) + (wk < owner ? wk : wk - 1)) * 64] = acc[u / NT][u % NT];
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < MT * NT; ++u) {
-        if (wk != u % WK) continue;
-        v4f sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g = 0; g < kGroups; ++g) {
+        const int owner = g % WK;
+        if (wk != owner) continue;
+        v4f sum[G];
 #pragma unroll
-        for (int p = 0; p < WK; ++p) {
-            const v4f v = p == u % WK ? acc[u / NT][u % NT] : parts[(u * (WK - 1) + (p < u % WK ? p : p - 1)) * 64];
+        for (int i = 0; i < G; ++i) {
+            const int u = g * G + i;
+            sum[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum[r] += v[r];
+            for (int p = 0; p < WK; ++p) {
+                const v4f v = p == owner ? acc[u / NT][u % NT] : parts[(u * (WK - 1) + (p < owner ? p : p - 1)) * 64];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[i][r] += v[r];
+            }
         }
-        const int row = row0 + 16 * (u / NT);
-        if (row < T) store4<BF16>(Y + (int64_t)row * ldy, col0 + 4 * (u % NT), O, sum, vec);
+        store(g * G, sum);
     }
 }
 
@@ -299,7 +305,7 @@ static_assert(kRingLds <= 160 * 1024, "LDS of a CU");
 template <int NT, bool BF16>
 __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const float* __restrict__ x_scale,
                                           const int8_t* __restrict__ qw, const float* __restrict__ w_scale, int T, int nk, int O,
-                                          uint16_t* __restrict__ Y, int64_t ldy, bool vec, bool vec8, int8_t* lds, int m0, int n0) {
+                                          uint16_t* __restrict__ Y, int64_t ldy, int8_t* lds, int m0, int n0) {
     constexpr int MT = 8, WN = 4, WTN = 16 * NT, kMidAt = 0, kLateAt = 3, kEarlyAt = 1, kAhead = 3;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -462,17 +468,14 @@ __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const f
 
     const int col0 = n0 + wn * WTN + 4 * NT * grp, row0 = m0 + wm * 128 + fr;
     // Outputs leave 16 bytes a lane, and whole lines of 128 bytes an instruction: of its 32 bytes of a token (NT = 4) a lane keeps one
-    // half and trades the other for the same half of its neighbour's token.  (4096 x 4096 x 4096: 8 bytes a lane 63.4 us, 16 of its own token 59.1, KLINES so)
+    // half and trades the other for the same half of its neighbour's token.  (4096 x 4096 x 4096: 8 bytes a lane 63.4 us, 16 of its own
+    // token 59.0, 57.4 so)
     const int odd = lane & 1;
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
         const int row = row0 + 16 * mi;
-        if (!vec8) {
-            if (row >= T) continue;
-#pragma unroll
-            for (int ni = 0; ni < NT; ++ni) store4<BF16>(Y + (int64_t)row * ldy, col0 + 4 * ni, O, acc[mi][ni], vec);
-        } else if (NT == 2) {
-            if (row < T) store8(Y + (int64_t)row * ldy, col0, O, pack8<BF16>(acc[mi][0], acc[mi][1]));
+        if (NT == 2) {
+            if (row < T) store_row(Y + (int64_t)row * ldy, col0, O, pack8<BF16>(acc[mi][0], acc[mi][1]));
         } else {
             const v4u lo = pack8<BF16>(acc[mi][0], acc[mi][1]), hi = pack8<BF16>(acc[mi][NT - 2], acc[mi][NT - 1]);
             v4u even, next;
@@ -483,8 +486,8 @@ __device__ __forceinline__ void ring_tile(const int8_t* __restrict__ qx, const f
                 next[i] = odd ? hi[i] : other;
             }
             uint16_t* y = Y + (int64_t)(row - odd) * ldy;
-            if (row - odd < T) store8(y, col0 + 8 * odd, O, even);
-            if (row - odd + 1 < T) store8(y + ldy, col0 + 8 * odd, O, next);
+            if (row - odd < T) store_row(y, col0 + 8 * odd, O, even);
+            if (row - odd + 1 < T) store_row(y + ldy, col0 + 8 * odd, O, next);
         }
     }
 }
@@ -494,7 +497,7 @@ template <bool BF16>
 __global__ void __launch_bounds__(64 * kSplitWaves, 2)
 gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale, const int8_t* __restrict__ qw,
                      const float* __restrict__ w_scale, int T, int nk, int O, uint16_t* __restrict__ Y, int64_t ldy, int tiles_m,
-                     int tiles_n, int n_whole, bool vec, bool vec8) {
+                     int tiles_n, int n_whole) {
     extern __shared__ __align__(16) int8_t lds[];
     const int whole_blocks = (n_whole + kXcds - 1) / kXcds * kXcds;
     const bool whole = (int)blockIdx.x < whole_blocks;
@@ -505,8 +508,8 @@ gemm_fp8_ring_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_
     tile_of_index(whole ? at : n_whole + at / 2, tiles_m, tiles_n, tile_m, tile_n);
     const int m0 = tile_m * kRingTile, n0 = tile_n * kRingTile + (whole ? 0 : at % 2 * (kRingTile / 2));
     if (n0 >= O) return;                                      // the right half of a last tile may have no channel
-    if (whole) ring_tile<4, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, vec8, lds, m0, n0);
-    else ring_tile<2, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, vec, vec8, lds, m0, n0);
+    if (whole) ring_tile<4, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, lds, m0, n0);
+    else ring_tile<2, BF16>(qx, x_scale, qw, w_scale, T, nk, O, Y, ldy, lds, m0, n0);
 }
 
 hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const float* ws, int T, int nk, int O, uint16_t* Y, bool bf16,
@@ -517,12 +520,10 @@ hipError_t go_ring(const int8_t* qx, const float* xs, const int8_t* qw, const fl
     auto padded = [](int64_t n) { return (n + kXcds - 1) / kXcds * kXcds; };
     const int64_t blocks = padded(n_whole) + padded(halves);
     if (!grid_fits(blocks, 64 * kSplitWaves)) return hipErrorInvalidValue;
-    const bool vec = reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0;
-    const bool vec8 = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0;
     static std::atomic<uint64_t> done[2];
     auto launch = [&](auto k, std::atomic<uint64_t>& d) {
         if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kRingLds, d); e != hipSuccess) return e;
-        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, (int)n_whole, vec, vec8);
+        k<<<(unsigned)blocks, 64 * kSplitWaves, kRingLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, (int)n_whole);
         return hipGetLastError();
     };
     return bf16 ? launch(gemm_fp8_ring_kernel<true>, done[1]) : launch(gemm_fp8_ring_kernel<false>, done[0]);
@@ -535,13 +536,12 @@ hipError_t go(const int8_t* qx, const float* xs, const int8_t* qw, const float* 
     const int tiles_m = (T + P::TM - 1) / P::TM, tiles_n = (O + P::TN - 1) / P::TN;
     const int64_t total = (int64_t)tiles_m * tiles_n, blocks = (total + kXcds - 1) / kXcds * kXcds;
     if (!grid_fits(blocks, 64 * kSplitWaves)) return hipErrorInvalidValue;
-    const bool vec = reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0;
     static std::atomic<uint64_t> done[2];
     const void* kernel = bf16 ? reinterpret_cast<const void*>(gemm_fp8_kernel<MT, NT, WM, WN, WK, S, true>)
                               : reinterpret_cast<const void*>(gemm_fp8_kernel<MT, NT, WM, WN, WK, S, false>);
     if (hipError_t e = allow_dynamic_lds(kernel, P::kLds, done[bf16]); e != hipSuccess) return e;
     auto launch = [&](auto k) {
-        k<<<(unsigned)blocks, 64 * kSplitWaves, P::kLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n, vec);
+        k<<<(unsigned)blocks, 64 * kSplitWaves, P::kLds, stream>>>(qx, xs, qw, ws, T, nk, O, Y, ldy, tiles_m, tiles_n);
     };
     if (bf16) launch(gemm_fp8_kernel<MT, NT, WM, WN, WK, S, true>);
     else launch(gemm_fp8_kernel<MT, NT, WM, WN, WK, S, false>);
