@@ -215,6 +215,15 @@ def test_linear_by_other_tiles(cq, torch, T, I, O, kind):
     test_linear(cq, torch, T, I, O, kind)
 
 
+# weights of more than 128 MiB
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,I,O,kind", [(16, 8192, 16400, "bfloat16"), (30, 8192, 16400, "float16"), (60, 8192, 16400, "bfloat16"),
+                                        (100, 8192, 16400, "float16"), (5, 131200, 1030, "bfloat16"), (27, 131200, 1030, "float16"),
+                                        (50, 131200, 1100, "bfloat16")])
+def test_linear_with_large_weights(cq, torch, T, I, O, kind):
+    test_linear(cq, torch, T, I, O, kind)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("offset,pitch", [(0, 336), (0, 300), (4, 304), (1, 301), (2, 310)])
 @pytest.mark.parametrize("T", [5, 70, 260])
