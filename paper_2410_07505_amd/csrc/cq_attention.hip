@@ -86,6 +86,16 @@ struct Bytes {
             __builtin_memcpy(w, __builtin_assume_aligned(p, N < 16 ? N : 16), N);
         }
     }
+    // the same for bytes that no other load asks for and no cache keeps
+    __device__ __forceinline__ void load_once(const uint8_t* p) {
+        if (N == 2) return load(p);
+        typedef uint32_t V __attribute__((ext_vector_type(N < 4 ? 1 : N < 16 ? N / 4 : 4)));
+#pragma unroll
+        for (int i = 0; i < (N + 15) / 16; ++i) {
+            const V v = __builtin_nontemporal_load(reinterpret_cast<const V*>(p) + i);
+            __builtin_memcpy(w + 4 * i, &v, sizeof(v));
+        }
+    }
 };
 
 // Which of a lane's channels (neighbours, 16 or 32 at a time, see the queries' part) byte e of fragment f holds.  8 bits: fragment f is
@@ -152,7 +162,8 @@ struct Shared {
 };
 
 // Units [unit0, unit0 + count) of a pair.  piece < 0: that is all of it, and the result is written; otherwise where it goes.
-template <int DIM, int BITS, int MR>
+// ONCE: the values' loads are non-temporal.
+template <int DIM, int BITS, int MR, bool ONCE>
 __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, int64_t seq, int head, int rt, int n, int unit0, int count,
                                                 int piece) {
     constexpr int kFrags = DIM / 64, kOut = DIM / 16, kRowBytes = DIM * BITS / 8;
@@ -197,7 +208,11 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         for (int t = 0; t < kSub; ++t) {
             const uint8_t* vp = a.v_codes + k.row[t] * kRowBytes;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v.c[t][r].load(vp + (4 * grp + r) * kRowBytes + fr * ValuesT::kPiece);
+            for (int r = 0; r < 4; ++r) {
+                const uint8_t* at = vp + (4 * grp + r) * kRowBytes + fr * ValuesT::kPiece;
+                if (ONCE) v.c[t][r].load_once(at);
+                else v.c[t][r].load(at);
+            }
             const float4 f = *reinterpret_cast<const float4*>(a.v_scale + k.row[t] + 4 * grp);
             v.a[t][0] = f.x; v.a[t][1] = f.y; v.a[t][2] = f.z; v.a[t][3] = f.w;
         }
@@ -498,7 +513,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     }
 }
 
-template <int DIM, int BITS, int MR>
+template <int DIM, int BITS, int MR, bool ONCE>
 __global__ void __launch_bounds__(64 * kWaves, MR == 1 ? DIM == 64 ? 4 : DIM == 128 ? 3 : 2 : 2)
 attention_kernel(Args a) {
     __shared__ __align__(16) Shared<DIM> sh;
@@ -579,7 +594,7 @@ attention_kernel(Args a) {
             ends[2 * pair + 1] = count == u ? blockIdx.x : Cut(total, a.n_blocks).block_of(at + u - 1);
         }
         // a stretch has at most one piece that continues a pair and one that only begins one
-        attention_piece<DIM, BITS, MR>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
+        attention_piece<DIM, BITS, MR, ONCE>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
                                        count == u ? -1 : 2 * blockIdx.x + (unit == 0 ? 1 : 0));
         at += count;
         if (at >= end) break;
@@ -784,16 +799,26 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
     a.out = out; a.partial = workspace; a.n_partials = partials(c, s, p);
     a.heads = c.heads; a.group = group; a.S = s.S; a.row_tiles = p.row_tiles; a.n_blocks = p.n_blocks; a.n_sequences = s.B;
     a.page_shift = c.page_shift; a.max_length = s.max_length; a.scale = scale; a.bf16 = bf16;
-    auto go = [&](auto kernel) { kernel<<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a); };
-    if (c.bits == 8) {
-        if (c.dim == 64) p.mr == 2 ? go(attention_kernel<64, 8, 2>) : go(attention_kernel<64, 8, 1>);
-        else if (c.dim == 128) p.mr == 2 ? go(attention_kernel<128, 8, 2>) : go(attention_kernel<128, 8, 1>);
-        else go(attention_kernel<256, 8, 1>);
-    } else {
-        if (c.dim == 64) p.mr == 2 ? go(attention_kernel<64, 4, 2>) : go(attention_kernel<64, 4, 1>);
-        else if (c.dim == 128) p.mr == 2 ? go(attention_kernel<128, 4, 2>) : go(attention_kernel<128, 4, 1>);
-        else go(attention_kernel<256, 4, 1>);
-    }
+    // What the memory-side cache (256 MiB) cannot keep for the next call, beside another layer's, is not put there, as far as values go: a
+    // value row is loaded by one instruction, a key row by several.  64 x 1024-8192 133 -> 125 us, 2 x 131072 INT4 64.4 -> 59.8, 100
+    // sequences of 2048 62 -> 53, 32 of 4096 (16 heads of 64, 150 MiB) 45 -> 41; two caches of 127 MiB in turn, which stay there, 31.5 -> 33.
+    // (keys too: 128 us, 65, 62, 47)
+    const int64_t positions = std::min(s.B * (int64_t)s.max_length, c.pages << c.page_shift);
+    const bool once = positions * c.heads * 2 * (c.dim * c.bits / 8 + 4) > (int64_t)128 << 20;
+    auto go = [&](auto dim, auto bits, auto mr) {
+        constexpr int kDim = decltype(dim)::value, kBits = decltype(bits)::value, kMr = decltype(mr)::value;
+        if (once) attention_kernel<kDim, kBits, kMr, true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
+        else attention_kernel<kDim, kBits, kMr, false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
+    };
+    auto with_bits = [&](auto bits) {
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        if (c.dim == 64) p.mr == 2 ? go(std::integral_constant<int, 64>(), bits, Two()) : go(std::integral_constant<int, 64>(), bits, One());
+        else if (c.dim == 128) p.mr == 2 ? go(std::integral_constant<int, 128>(), bits, Two()) : go(std::integral_constant<int, 128>(), bits, One());
+        else go(std::integral_constant<int, 256>(), bits, One());
+    };
+    if (c.bits == 8) with_bits(std::integral_constant<int, 8>());
+    else with_bits(std::integral_constant<int, 4>());
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_blocks == 0) return e;
     auto join = [&](auto many, auto few) {
         if (rows >= 1024) many<<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(a, 16 * p.mr, rows);

@@ -362,6 +362,22 @@ def test_attention_of_many_sequences(cq, torch, B, longest, S, heads, group, dim
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits,heads,dim,group,kind", [(8, 8, 128, 4, "float16"), (8, 16, 64, 20, "bfloat16"), (8, 4, 256, 2, "bfloat16"),
+                                                       (4, 8, 256, 3, "float16"), (4, 16, 128, 20, "bfloat16"), (4, 16, 64, 1, "float16")])
+def test_attention_over_a_large_cache(cq, torch, bits, heads, dim, group, kind):
+    """Calls that could read more than 128 MiB, as their max_length says."""
+    page = 64
+    pages = -(-(130 << 20) // (2 * heads * (dim * bits // 8 + 4) * page))
+    lengths = [3000, 0, 1, 1700, 64, 129, 20, 2500, 333]
+    cache = make_cache(torch, cq, bits, pages, heads, page, dim, seed=31)
+    table, lens = make_table(torch, cache, lengths, seed=31, extra=-(-pages // len(lengths)))
+    assert len(lengths) * table.shape[1] >= pages
+    Q = queries(torch, len(lengths), 1, heads * group, dim, kind, 31) / float(cache.k_col.mean())
+    out = check_attention(torch, cq, cache, Q, table, lens)
+    assert torch.equal(out, cq.crossquant_cache_attention(cache, Q, table, lens))
+
+
+@pytest.mark.gpu
 def test_two_graphs_and_eager_calls_of_attention_at_once(cq, torch):
     """Two graphs of one cache, each with its own workspace, on streams of their own beside eager calls; lengths and table change
     between replays."""
