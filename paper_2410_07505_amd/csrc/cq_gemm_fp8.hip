@@ -295,8 +295,9 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
 //     and the first of step k + 2 are requested in step k, into the place that step k - 1 left and the one that was free;
 //   token scales: three slots of 1 KiB.
 // Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us; two a product, by all
-// waves, 857; this form 790 to 840, 2.3 to 2.4 PFLOP/s.  With operands of zeros it takes 693: the difference is the clock under power,
-// 1.9 GHz.  Matrix instructions alone from registers reach 4.5 PFLOP/s; what remains are the instructions a wave has to issue between
+// waves, 857; this form 790 to 810, 780 with whole-line stores, 2.45 PFLOP/s.  With operands of zeros it took 690: the difference is the
+// clock under power, 1.8 GHz.  Without the requests of all steps but the first it would take 666 (zeros: 568), without the additions 723.
+// Matrix instructions alone from registers reach 4.5 PFLOP/s; what remains are the instructions a wave has to issue between
 // them (reads of fragments, additions, requests).
 //
 // NT = 2 is half a tile, 256 x 128 (128 x 32 a wave, half the weight requests): outputs of less than a round of the CUs, and the last
