@@ -239,6 +239,25 @@ def test_linear_into_padded_rows(cq, torch, T, offset, pitch):
     assert (store[untouched] == 77.0).all()
 
 
+# outputs at every alignment, by every way to tile a layer, against those of an aligned buffer; nothing else is written
+@pytest.mark.gpu
+@pytest.mark.parametrize("extra", [0, 1, 2, 5])
+@pytest.mark.parametrize("T,I,O", [(2000, 128, 11001), (1000, 1024, 4102), (513, 384, 4101), (300, 384, 4099), (64, 512, 4103), (17, 384, 8201),
+                                   (1, 384, 8203), (4, 256, 70), (16, 2048, 2101)])
+def test_linear_into_rows_of_odd_pitch(cq, torch, T, I, O, extra):
+    qx, xs, qw, ws = operands(torch, T, I, O, T + O)
+    want = torch.empty((T, (O + 7) // 8 * 8), dtype=torch.bfloat16, device="cuda")[:, :O]
+    cq.crossquant_fp8_linear(qx, xs, qw, ws, Y=want)
+    assert torch.isfinite(want).all()
+    pitch = O + extra
+    store = torch.full((T * pitch + 64,), 77.0, dtype=torch.bfloat16, device="cuda")
+    Y = store[extra:extra + T * pitch].view(T, pitch)[:, :O]
+    cq.crossquant_fp8_linear(qx, xs, qw, ws, Y=Y)
+    assert torch.equal(Y, want)
+    store[extra:extra + T * pitch].view(T, pitch)[:, :O] = 77.0
+    assert (store == 77.0).all()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_linear_at_the_ends_of_the_formats(cq, torch, T):
