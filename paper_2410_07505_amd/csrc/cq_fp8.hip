@@ -84,15 +84,22 @@ quantize_fp8_kernel(const uint16_t* __restrict__ X, int T, int I, int64_t ldx, i
     if (row < R && t0 + row < T) scale[(int64_t)(j / kGroup) * T + t0 + row] = mine;
 }
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 // One block of 256 threads for one 128 x 128 block of W [I][O]; the codes leave transposed, [O][Ip].
-// A thread holds 8 rows x 8 columns.  The 16 lanes of a row of lanes hold the 128 rows of the same 8 columns, so that the codes
-// of a column leave as 128 adjacent bytes, 8 a lane; their loads are 64 adjacent bytes of 16 rows.
+// A thread holds 8 rows x 8 columns, 16 lanes the 128 columns of the same rows: a load is 256 adjacent bytes of four rows.  The codes of a
+// column's 8 rows, 8 bytes, pass through LDS ([column][16 chunks], chunk q of column group g at q ^ g, which spreads writes and reads over
+// the banks), so that a column's 128 leave as a whole line, 16 bytes a lane, and past the caches: a weight is prepared long before it is
+// used.  (4096 x 11008, 8192 x 28672, 4096 x 4096, 2750 x 4090: rows of 64 bytes loaded and 8 bytes a lane stored, without LDS 34.9,
+// 147, 10.8 and 10.5 us; through LDS 32.8, 138, 11.1 and 10.9; past the caches too 25.6, 131, 9.3 and 9.8, 5.3 TB/s.)
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(256)
 weight_fp8_kernel(const uint16_t* __restrict__ W, int I, int O, int nb, uint8_t* __restrict__ qw, float* __restrict__ w_scale) {
     __shared__ uint32_t part[4];
+    __shared__ __align__(16) uint2 tile[kGroup][16];
     const int b = blockIdx.x % nb, ob = blockIdx.x / nb;
-    const int i0 = b * kGroup + 8 * (threadIdx.x & 15), o0 = ob * kGroup + 8 * (threadIdx.x >> 4);
+    const int g = threadIdx.x & 15, q = threadIdx.x >> 4;
+    const int i0 = b * kGroup + 8 * q, o0 = ob * kGroup + 8 * g;
     const int64_t Ip = (int64_t)nb * kGroup;
     uint4 v[8];
 #pragma unroll
@@ -112,15 +119,20 @@ weight_fp8_kernel(const uint16_t* __restrict__ W, int I, int O, int nb, uint8_t*
     if (threadIdx.x == 0) w_scale[(int64_t)ob * nb + b] = sc.s;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        if (o0 + c >= O) break;
         float f[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             const uint32_t w = c < 2 ? v[r].x : c < 4 ? v[r].y : c < 6 ? v[r].z : v[r].w;
             f[r] = (c & 1 ? hi_f<BF16>(w) : lo_f<BF16>(w)) * sc.r;
         }
-        *reinterpret_cast<uint2*>(qw + (int64_t)(o0 + c) * Ip + i0) =
-            make_uint2(four_codes(f[0], f[1], f[2], f[3]), four_codes(f[4], f[5], f[6], f[7]));
+        tile[8 * g + c][q ^ g] = make_uint2(four_codes(f[0], f[1], f[2], f[3]), four_codes(f[4], f[5], f[6], f[7]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int col = 32 * c + (threadIdx.x >> 3), o = ob * kGroup + col, h = 2 * (threadIdx.x & 7);
+        const uint2 x = tile[col][h ^ (col >> 3)], y = tile[col][(h + 1) ^ (col >> 3)];
+        if (o < O) __builtin_nontemporal_store(v4u{x.x, x.y, y.x, y.y}, reinterpret_cast<v4u*>(qw + (int64_t)o * Ip + b * kGroup + 8 * h));
     }
 }
 
