@@ -109,6 +109,13 @@ def test_activation_codes(cq, torch, T, I, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,I,kind", [(2051, 4100, "float16"), (16385, 513, "bfloat16"), (4097, 2041, "float16")])
+def test_activation_codes_of_many_rows(cq, torch, T, I, kind):
+    """Several rows a wave, an odd number of them."""
+    test_activation_codes(cq, torch, T, I, kind)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("offset,pitch", [(0, 776), (8, 768), (1, 768), (3, 777)])
 def test_activation_codes_of_strided_rows(cq, torch, offset, pitch):
     X = activation(torch, 40, 700, "bfloat16", 5)
