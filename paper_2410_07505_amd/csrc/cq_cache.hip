@@ -214,17 +214,18 @@ hipError_t dispatch(const CacheView& c, bool bf16, F f) {
     return hipGetLastError();
 }
 
-// Rows a thread takes, and blocks for the keys of T tokens: four rows, where that leaves `least` blocks.  Four share a head's
-// factors, a wait and, in the write, one power: INT4, 2 x 8 heads of 128, 16384 tokens are written in 27.5 us and read in 14.9
-// (5.7 TB/s), with one row 31.7 and 16.5; with fewer blocks than that one row a thread hides more of the latency (64 tokens, written:
-// 3.0 us with one, 5.8 with four; between 128 and 1024 blocks the two are within 3 %).
+// Rows a thread takes, and blocks for the keys of T tokens: `many` rows where that leaves `least` blocks, else one.  Several share a
+// head's factors, a wait and, in the write, one power: INT4, 2 x 8 heads of 128, 16384 tokens are written in 24.5 us with eight, 27.6
+// with four and 31.7 with one, and read in 14.9 with four (5.7 TB/s), 14.6 with eight and 16.5 with one (INT8, 8192 tokens: 9.4, 10.2
+// and 10.3).  With fewer blocks one row a thread hides more of the latency (64 tokens, written: 3.0 us with one, 5.8 with four;
+// from 2048 to 4096 tokens all are within 3 %).
 struct Stretches {
     int rows;
     int64_t blocks;
 };
-Stretches stretches(const CacheView& c, int T, int64_t least) {
-    const int64_t kept = 256 / (c.dim / 8), four = (T + 4 * kept - 1) / (4 * kept) * c.heads;
-    if (four >= least) return {4, four};
+Stretches stretches(const CacheView& c, int T, int many, int64_t least) {
+    const int64_t kept = 256 / (c.dim / 8), blocks = (T + many * kept - 1) / (many * kept) * c.heads;
+    if (blocks >= least) return {many, blocks};
     return {1, (T + kept - 1) / kept * c.heads};
 }
 
@@ -232,21 +233,21 @@ Stretches stretches(const CacheView& c, int T, int64_t least) {
 
 hipError_t launch_cache_write(const CacheView& c, const uint16_t* K, int64_t k_token, int64_t k_head, const uint16_t* V,
                               int64_t v_token, int64_t v_head, bool bf16, const int32_t* slots, int T, hipStream_t stream) {
-    const Stretches g = stretches(c, T, 512);
+    const Stretches g = stretches(c, T, 8, 512);
     if (!grid_fits(2 * g.blocks, 256)) return hipErrorInvalidValue;
     return dispatch(c, bf16, [&](auto dim, auto bits, auto bf) {
         auto go = [&](auto kernel) {
             kernel<<<dim3((unsigned)g.blocks, 2), 256, 0, stream>>>(side_k(c), side_v(c), Source{K, k_token, k_head}, Source{V, v_token, v_head},
                                                                     slots, T, c.heads, c.page_shift, c.pages << c.page_shift, c.alpha);
         };
-        if (g.rows == 4) go(cache_write_kernel<dim(), bits(), bf(), 4>);
+        if (g.rows == 8) go(cache_write_kernel<dim(), bits(), bf(), 8>);
         else go(cache_write_kernel<dim(), bits(), bf(), 1>);
     });
 }
 
 hipError_t launch_cache_read(const CacheView& c, const int32_t* slots, int T, uint16_t* K, uint16_t* V, bool bf16,
                              hipStream_t stream) {
-    const Stretches g = stretches(c, T, 1024);
+    const Stretches g = stretches(c, T, 4, 1024);
     if (!grid_fits(2 * g.blocks, 256)) return hipErrorInvalidValue;
     return dispatch(c, bf16, [&](auto dim, auto bits, auto bf) {
         auto go = [&](auto kernel) {

@@ -217,6 +217,13 @@ def test_write_and_read_of_many_rows(cq, torch, T, heads, dim, page, bits, kind)
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,heads,dim,page,bits,kind", [(4101, 32, 64, 64, 8, "bfloat16"), (4099, 17, 128, 64, 4, "float16"), (2051, 17, 256, 64, 8, "float16"),
+                                                       (2060, 32, 128, 64, 4, "bfloat16"), (4200, 32, 64, 16, 4, "float16"), (2049, 17, 256, 32, 4, "bfloat16")])
+def test_write_and_read_of_more_rows(cq, torch, T, heads, dim, page, bits, kind):
+    test_write_and_read(cq, torch, T, heads, dim, page, 0.6, True, bits, kind)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [3, 2000])
 @pytest.mark.parametrize("bits,kind", [(8, "float16"), (8, "bfloat16"), (4, "float16"), (4, "bfloat16")])
 def test_write_of_quotients_near_ties(cq, torch, bits, kind, T):
