@@ -71,7 +71,7 @@ def _build_fastcall() -> None:
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            '-DCQ_TORCH_VERSION="%s"' % _torch_version(torch),
            *("-I" + i for i in includes), os.path.join(CSRC, "cq_fastcall.cpp"), "-o", tmp,
-           "-L" + os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+           "-L" + os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed for cq_fastcall.cpp:\n" + res.stdout)
