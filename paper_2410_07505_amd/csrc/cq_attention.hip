@@ -155,18 +155,18 @@ __device__ __forceinline__ int64_t scalar(int64_t v) {
     return (int64_t)((uint64_t)(uint32_t)scalar((int)(v >> 32)) << 32 | (uint32_t)scalar((int)v));
 }
 
-template <int DIM>
+template <int DIM, int W>
 struct Shared {
-    float o[kWaves][16][DIM + 4];                          // 16 rows 4 banks apart
-    float ml[kWaves][16][2];
+    float o[W][16][DIM + 4];                               // 16 rows 4 banks apart
+    float ml[W][16][2];
 };
 
 // Units [unit0, unit0 + count) of a pair.  piece < 0: that is all of it, and the result is written; otherwise where it goes.
-// ONCE: the values' loads are non-temporal.
-template <int DIM, int BITS, int MR, bool ONCE>
-__device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, int64_t seq, int head, int rt, int n, int unit0, int count,
+// ONCE: the values' loads are non-temporal.  W: waves of the block (a unit is W tiles of positions).
+template <int DIM, int BITS, int MR, bool ONCE, int W>
+__device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& sh, int64_t seq, int head, int rt, int n, int unit0, int count,
                                                 int piece) {
-    constexpr int kFrags = DIM / 64, kOut = DIM / 16, kRowBytes = DIM * BITS / 8;
+    constexpr int kFrags = DIM / 64, kOut = DIM / 16, kRowBytes = DIM * BITS / 8, kStep = W * kTile;
     using KeysT = Keys<DIM, BITS>;
     using ValuesT = Values<DIM, BITS>;
 
@@ -175,7 +175,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     const int rows = a.S * a.group, row0 = rt * 16 * MR, tile_rows = min(16 * MR, rows - row0);
     const int s_first = row0 / a.group, s_last = (row0 + tile_rows - 1) / a.group;
     const int see_min = visible(a, n, s_first), see_max = visible(a, n, s_last);
-    const int begin = unit0 * kBlockStep, end = min(begin + count * kBlockStep, see_max);
+    const int begin = unit0 * kStep, end = min(begin + count * kStep, see_max);
 
     // ---- loads of a tile's positions from `pos`.  Positions on no page read page 0 and are masked.
     const int32_t* table = a.table + seq * a.table_width;
@@ -184,8 +184,8 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     // would stand in front of every tile's loads.
     static_assert(kSub == 2, "two lanes a tile");
     int pages = -1;
-    auto load_pages = [&](int pos) {                       // of the tiles at pos, pos + kBlockStep, ..
-        const int64_t p = pos + (int64_t)(lane >> 1) * kBlockStep + 16 * (lane & 1);
+    auto load_pages = [&](int pos) {                       // of the tiles at pos, pos + kStep, ..
+        const int64_t p = pos + (int64_t)(lane >> 1) * kStep + 16 * (lane & 1);
         pages = p < see_max ? table[min((int)(p >> a.page_shift), last_page)] : -1;
     };
     auto load_keys = [&](KeysT& k, int pos, int tile) {
@@ -298,7 +298,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     // Keys are requested for the next positions as soon as the scores are out, values as soon as they are summed: one set of registers
     // each, and always something on its way.
     while (pos < end) {
-        const int next = pos + kBlockStep;
+        const int next = pos + kStep;
         bool off[kSub], masked = pos + kTile > see_min;        // (scalar)
 #pragma unroll
         for (int t = 0; t < kSub; ++t) {
@@ -473,16 +473,16 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
         __syncthreads();
         constexpr int kCols = DIM / 16;                    // channels a thread joins
         const int row = threadIdx.x / 16, d0 = threadIdx.x % 16 * kCols, in_tile = 16 * mr + row;
-        if (in_tile >= tile_rows) continue;
+        if (in_tile >= tile_rows || row >= 16) continue;
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][row][0]);
+        for (int w = 0; w < W; ++w) top = fmaxf(top, sh.ml[w][row][0]);
         const float ref = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, acc[kCols];
 #pragma unroll
         for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float f = __builtin_amdgcn_exp2f(sh.ml[w][row][0] - ref);
             total = __builtin_fmaf(f, sh.ml[w][row][1], total);
 #pragma unroll
@@ -513,15 +513,16 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM>& sh, 
     }
 }
 
-template <int DIM, int BITS, int MR, bool ONCE>
-__global__ void __launch_bounds__(64 * kWaves, MR == 1 ? DIM == 64 ? 4 : DIM == 128 ? 3 : 2 : 2)
+// W = 8: a block a pair only.
+template <int DIM, int BITS, int MR, bool ONCE, int W>
+__global__ void __launch_bounds__(64 * W, MR == 1 ? DIM == 64 ? 4 : DIM == 128 ? 3 : 2 : 2)
 attention_kernel(Args a) {
-    __shared__ __align__(16) Shared<DIM> sh;
+    __shared__ __align__(16) Shared<DIM, W> sh;
     __shared__ int64_t sh_sum[kWaves], sh_at[2];
     const int per_seq = a.heads * a.row_tiles, tid = threadIdx.x;          // pairs of a sequence
     int64_t total = 0, at = 0, end = 0;
     int seq, j, unit, n, u;
-    if (a.n_blocks == 0) {
+    if (W != kWaves || a.n_blocks == 0) {
         seq = blockIdx.x / per_seq;
         j = blockIdx.x - seq * per_seq;
         unit = 0;
@@ -594,7 +595,7 @@ attention_kernel(Args a) {
             ends[2 * pair + 1] = count == u ? blockIdx.x : Cut(total, a.n_blocks).block_of(at + u - 1);
         }
         // a stretch has at most one piece that continues a pair and one that only begins one
-        attention_piece<DIM, BITS, MR, ONCE>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
+        attention_piece<DIM, BITS, MR, ONCE, W>(a, sh, seq, j / a.row_tiles, j % a.row_tiles, n, unit, count,
                                        count == u ? -1 : 2 * blockIdx.x + (unit == 0 ? 1 : 0));
         at += count;
         if (at >= end) break;
@@ -754,14 +755,18 @@ attention_join_kernel(Args a, int rows_per_tile) {
 // needs no second kernel.  A unit that follows another in a block takes some 1 us, the second kernel and finding the stretches 4, so
 // a block a pair is for pairs of at most
 // - four units: one sequence (8 pairs) of 256 (500) positions 8.4 (10.5) us so, 11.6 (11.7) in stretches, 640 positions 11.4 and 11.8;
-// - eight where they keep half the CUs busy: of up to 1024 positions, 16 sequences 17.0 and 18.8, 100 31 and 40, 200 67 and 77;
-// - sixteen where they fill the chip: of up to 2048 positions, 100 sequences 62 and 68, 400 211 and 224;
+// - sixteen where they keep half the CUs busy: of up to 1024 positions, 100 sequences 31 and 40, 200 67 and 77; of up to 2048, 60
+//   37 and 40, 100 62 and 68, 400 211 and 224;
 // - what each of the chip's places gets of them where that is more still.
+// Pairs of more than four units that do not fill the CUs twice have blocks of eight waves, half the steps: 16 sequences of up to 1024
+// (2048) positions 14.9 (21.3) us, with four waves 16.9, in stretches 18.8 (24.2); 30: 15.9 (22.7), 17.5, (29.4).  With four units the
+// longer way to one result costs as much: 10.7 and 10.5; with more pairs eight waves are in each other's way: 48 of 1024 24.6 and 21.3.
 // Lengths are known on the GPU only: longer ones could keep all others waiting (1024 sequences of 4096 positions, INT4, of about one
 // length: 578 and 607).
 struct Plan {
     int mr, row_tiles, n_blocks;
     int64_t pairs;
+    bool wide;                                             // eight waves a block
 };
 Plan plan(const CacheView& c, const AttentionShape& s) {
     Plan p;
@@ -771,7 +776,8 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.pairs = s.B * c.heads * p.row_tiles;
     p.n_blocks = p.mr > 1 || c.dim == 256 ? 512 : c.dim == 128 ? 768 : 1024;
     const int64_t longest = (s.max_length + (int64_t)kBlockStep - 1) / kBlockStep;
-    if (longest <= (p.pairs < 128 ? 4 : p.pairs < p.n_blocks ? 8 : std::max<int64_t>(16, p.pairs / p.n_blocks))) p.n_blocks = 0;
+    if (longest <= (p.pairs < 128 ? 4 : std::max<int64_t>(16, p.pairs / p.n_blocks))) p.n_blocks = 0;
+    p.wide = p.n_blocks == 0 && longest > 4 && p.pairs <= 256;
     return p;
 }
 int64_t partials(const CacheView& c, const AttentionShape& s, const Plan& p) {
@@ -807,8 +813,9 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
     const bool once = positions * c.heads * 2 * (c.dim * c.bits / 8 + 4) > (int64_t)128 << 20;
     auto go = [&](auto dim, auto bits, auto mr) {
         constexpr int kDim = decltype(dim)::value, kBits = decltype(bits)::value, kMr = decltype(mr)::value;
-        if (once) attention_kernel<kDim, kBits, kMr, true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
-        else attention_kernel<kDim, kBits, kMr, false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
+        if (p.wide) attention_kernel<kDim, kBits, kMr, false, 8><<<(unsigned)blocks, 64 * 8, 0, stream>>>(a);
+        else if (once) attention_kernel<kDim, kBits, kMr, true, kWaves><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
+        else attention_kernel<kDim, kBits, kMr, false, kWaves><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a);
     };
     auto with_bits = [&](auto bits) {
         using One = std::integral_constant<int, 1>;

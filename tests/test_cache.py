@@ -355,6 +355,16 @@ def test_attention(cq, torch, case, bits, kind):
     (900, 200, 1, 7, 1, 128, 16, 8, "float16"),                # a block a pair
     (600, 160, 1, 7, 1, 256, 32, 4, "float16"),
     (520, 300, 2, 4, 10, 64, 16, 8, "bfloat16"),
+    (70, 2300, 1, 2, 7, 256, 32, 8, "bfloat16"),               # in pieces
+    (40, 2400, 2, 4, 9, 64, 64, 4, "float16"),
+    (200, 2100, 1, 2, 5, 128, 16, 8, "float16"),
+    (64, 2000, 1, 2, 4, 128, 64, 8, "float16"),                # wide blocks
+    (32, 1025, 1, 4, 4, 128, 16, 4, "bfloat16"),
+    (64, 600, 2, 4, 10, 64, 16, 8, "float16"),
+    (130, 1500, 1, 1, 1, 64, 32, 4, "bfloat16"),
+    (50, 1700, 3, 5, 6, 256, 64, 8, "bfloat16"),
+    (43, 1300, 1, 3, 17, 128, 32, 8, "bfloat16"),
+    (20, 1900, 4, 8, 8, 256, 16, 4, "float16"),
 ])
 def test_attention_of_many_sequences(cq, torch, B, longest, S, heads, group, dim, page, bits, kind):
     print("attention of %d sequences up to %d, %d x %d heads of %d" % (B, longest, heads, group, dim), flush=True)
