@@ -343,7 +343,8 @@ int crossquant_fp8_linear(const void *qx, const float *x_scale, const void *qw, 
  *
  * The cache is `pages` pages of page_size places.  Place `slot` is place slot % page_size of page slot / page_size.
  *   k_codes, v_codes: bits 8: int8 [pages][heads][page_size][dim]; bits 4: packed nibbles [pages][heads][page_size][dim / 2], even
- *     column in the low nibble.  16-byte aligned.  k_scale, v_scale: float [pages][heads][page_size], the rows' factors a.
+ *     column in the low nibble.  16-byte aligned.  k_scale, v_scale: float [pages][heads][page_size], the rows' factors a.  Who fills a
+ *     cache by other means writes factors that are finite and not negative, or NaN for a row that holds no number: not infinite.
  *   k_col, v_col: nullable, float [heads][dim], 16-byte aligned: the column factors b.
  *   dim is 64, 128 or 256; page_size a power of two from 16 to 65536 (else CQ_ERR_UNSUPPORTED); pages * page_size < 2^31.
  */
@@ -360,7 +361,7 @@ typedef struct {
  * Quantizes keys and values K, V [T][heads][dim] (type `type`; token i's row of head h starts at i * token_stride + h * head_stride
  * elements; 16-byte aligned with strides that are multiples of 8, else CQ_ERR_ALIGN) into the places slots[i], int32 [T].
  * A slot that is negative or past the cache writes nothing (padding tokens).  No other place is touched.
- * A row with an infinity or NaN gets a factor that is none either (alpha > 0): no value that it stands for is finite.
+ * A row with an infinity or NaN gets the factor NaN, for every alpha: all that it stands for is NaN, and so is each score with its key.
  * A slot may occur once in a call: of several tokens with the same slot, what the place holds afterwards is undefined.
  */
 int crossquant_cache_write(const cq_cache *cache, const void *K, int64_t k_token_stride, int64_t k_head_stride, const void *V,

@@ -1,7 +1,8 @@
 // Key/value cache in CrossQuant codes: quantized row by row as it is written, and read back.
 //
 //   a row is the `dim` channels of one token and head: t = max |x|, a = fl32(t^alpha / q_max), D_j = fl32(a b_j),
-//   q_j = D_j == 0 ? 0 : clamp(rne(fl32(x_j / D_j)), +-q_max);  read back: fl32(q_j D_j), rounded to the type asked for
+//   q_j = D_j == 0 ? 0 : clamp(rne(fl32(x_j / D_j)), +-q_max);  read back: fl32(q_j D_j), rounded to the type asked for;
+//   a = NaN for a row that holds an infinity or NaN
 // with the column factors b_j calibrated beforehand.  dim / 8 lanes take a row, 16 bytes of activations a lane.
 // Bound by memory for a prompt's worth of rows and by the latency of two dependent reads (slot, row) for a decode step's.
 #include "cq_device.h"
@@ -119,8 +120,10 @@ cache_write_kernel(Side ks, Side vs, Source k, Source v, const int32_t* __restri
         m_any = max(m_any, m);
         if (R == 1 || mine == i) m_mine = m;
     }
-    plain = plain & (m_any < (BF16 ? 0x7F80u : 0x7C00u));
-    const float a_mine = row_factor(BF16 ? __uint_as_float(m_mine << 16) : h2f(m_mine), alpha, kQmax);
+    constexpr uint32_t kInfinity = BF16 ? 0x7F80u : 0x7C00u;
+    plain = plain & (m_any < kInfinity);
+    // (an infinite factor would let a score of one sign drop out of the softmax as if the position were not there)
+    const float a_mine = m_mine < kInfinity ? row_factor(BF16 ? __uint_as_float(m_mine << 16) : h2f(m_mine), alpha, kQmax) : __builtin_nanf("");
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const float a = R == 1 ? a_mine : __shfl(a_mine, i, kLanesPerRow);

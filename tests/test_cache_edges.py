@@ -1,0 +1,63 @@
+"""The quantized cache where single numbers decide: rows that hold no number."""
+from __future__ import annotations
+
+import pytest
+
+from test_cache import cq, make_cache, make_table, queries, torch  # noqa: F401 (fixtures)
+
+
+# ---- rows that hold no number --------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("T,bits,kind,alpha", [(4, 8, "float16", 0.3), (4200, 8, "float16", 0.3), (3, 4, "bfloat16", 1.0), (4200, 4, "bfloat16", 1.0),
+                                               (5, 8, "bfloat16", 0.0), (4300, 4, "float16", 0.0)])
+def test_a_row_with_no_number_has_no_factor(cq, torch, T, bits, kind, alpha, value):
+    """Its factor is NaN whatever alpha is (one row a thread, and eight); all other rows are as without it."""
+    heads, dim, page = 33, 64, 16
+    cache = make_cache(torch, cq, bits, T // page + 1, heads, page, dim, alpha=alpha, seed=4)
+    X = torch.randn((T, heads, dim), generator=torch.Generator().manual_seed(6)).to(getattr(torch, kind)).cuda()
+    slots = torch.arange(T, dtype=torch.int32).cuda()
+    cq.crossquant_cache_write(cache, X, X, slots)
+    before = {n: getattr(cache, n).clone() for n in ("k_codes", "k_scale", "v_codes", "v_scale")}
+    K = X.clone()
+    K[T // 2, 2, 11] = value
+    cq.crossquant_cache_write(cache, K, X, slots)
+    at = (T // 2 // page, 2, T // 2 % page)
+    assert torch.isnan(cache.k_scale[at])
+    cache.k_scale[at], cache.k_codes[at] = before["k_scale"][at], before["k_codes"][at]
+    for n, t in before.items():
+        assert torch.equal(getattr(cache, n), t)
+
+
+# (lengths, key/value heads, query heads of each, tokens, dim, page, max_length): a block a pair, of four and of eight waves; two
+# register tiles of rows; in pieces, joined by half waves and by blocks
+FORMS = [([40, 3], 2, 8, 1, 64, 16, 40), ([600] * 64, 2, 2, 1, 128, 64, 600), ([90, 50], 1, 20, 2, 128, 32, 100),
+         ([1500, 30], 2, 6, 1, 256, 64, None), ([2500, 600, 30], 2, 4, 3, 128, 16, None), ([1300] * 70, 1, 20, 1, 64, 32, 2100)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("bits,kind", [(8, "float16"), (4, "bfloat16")])
+@pytest.mark.parametrize("form", range(len(FORMS)))
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_an_infinite_key_or_value_shows(cq, torch, side, form, bits, kind, value):
+    """Queries of either sign: all rows that see the place are NaN, no other row changes."""
+    lengths, heads, group, S, dim, page, max_length = FORMS[form]
+    cache = make_cache(torch, cq, bits, sum(-(-n // page) for n in lengths) + 1, heads, page, dim, seed=form)
+    table, lens = make_table(torch, cache, lengths, seed=form, extra=30)
+    Q = queries(torch, len(lengths), S, heads * group, dim, kind, form)
+    Q[:, :, 1::2] = -Q[:, :, ::2]
+    pos = lengths[0] * 2 // 3
+    slots = (table[0, pos // page] * page + pos % page).view(1)
+    X = torch.randn((1, heads, dim), generator=torch.Generator().manual_seed(form)).to(getattr(torch, kind)).cuda()
+    bad = X.clone()
+    bad[0, 0, 5] = value
+    cq.crossquant_cache_write(cache, X, X, slots)
+    want = cq.crossquant_cache_attention(cache, Q, table, lens, max_length=max_length)
+    assert torch.isfinite(want).all()
+    cq.crossquant_cache_write(cache, *((bad, X) if side == "k" else (X, bad)), slots)
+    out = cq.crossquant_cache_attention(cache, Q, table, lens, max_length=max_length)
+    assert torch.isnan(out[0, :, :group]).all()
+    out[0, :, :group] = want[0, :, :group]
+    assert torch.equal(out, want)
