@@ -378,8 +378,9 @@ int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T
  * in the cache already:
  *   out[b][s][h] = sum_p softmax_p(scale * q . k_p) v_p over the positions p < min(lengths[b] - (S - 1 - s), max_length)
  * with k_p, v_p of head h / (q_heads / heads) in binary32 from the codes.  Position p of sequence b is place p % page_size of page
- * page_table[b][p / page_size].  A row that sees no position (lengths[b] too small, or negative) is zero.  Positions on a page that is negative or past the
- * cache are not seen, and entries of the table behind the last visible position are not read; so are codes and scales there.
+ * page_table[b][p / page_size].  A row that sees no position (lengths[b] too small, or negative) is zero, whatever its query holds.  Positions
+ * on a page that is negative or past the cache are not seen, and entries of the table behind the last visible position are not read; so are
+ * codes and scales there.  A query that holds an infinity or NaN makes its row NaN.
  * Q, out: type `type`; Q: token s of sequence b at b * q_batch_stride + s * q_token_stride, head h another h * q_head_stride
  *   elements on (16-byte aligned, strides multiples of 8, else CQ_ERR_ALIGN); out: [B][S][q_heads][dim], contiguous, 16-byte aligned.
  * q_heads: a multiple of the cache's heads.  page_table: int32 [B][table_width]; lengths: int32 [B].

@@ -261,13 +261,21 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
         }
         top = max_groups(top);
         bad = sum_groups(bad);
-        const bool live = top >= kSmallest;                // kDigits / top stays in range
+        // A row whose query holds no number: digits of zero and an infinite factor, so that a score is 0 * infinity = NaN where the row
+        // sees the position and -infinity where it does not (a row that sees none stays zero).
+        const bool none = bad != 0.0f;
+        if (__any(none)) {
+            asm volatile("");                              // (a branch: seldom)
+#pragma unroll
+            for (int e = 0; e < kRuns * kRun; ++e) x[e] = none ? 0.0f : x[e];
+        }
+        const bool live = top >= kSmallest && !none;       // kDigits / top stays in range
         // a score is the digits' product times a factor that is never negative (the digits take the scale's sign) nor zero (which times
         // the -infinity of an unseen position would be no number)
         const float inv = live ? (a.scale < 0.0f ? -kDigits : kDigits) / top : 0.0f;
         // (codes of 4 bits enter as 16 times their value)
         const float f = (live ? top / kDigits : 0.0f) * (fabsf(a.scale) * 1.4426950408889634f * (BITS == 4 ? 0.0625f : 1.0f));
-        row_factor[mr] = fmaxf(f, 1.1754943508222875e-38f) + bad;
+        row_factor[mr] = none ? INFINITY : fmaxf(f, 1.1754943508222875e-38f);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
 #pragma unroll

@@ -1,4 +1,4 @@
-"""The quantized cache where single numbers decide: rows that hold no number."""
+"""The quantized cache where single numbers decide: rows that hold no number, tokens that see nothing."""
 from __future__ import annotations
 
 import pytest
@@ -61,3 +61,43 @@ def test_an_infinite_key_or_value_shows(cq, torch, side, form, bits, kind, value
     assert torch.isnan(out[0, :, :group]).all()
     out[0, :, :group] = want[0, :, :group]
     assert torch.equal(out, want)
+
+
+# ---- tokens that see nothing ---------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("bits,heads,group,dim,lengths,max_length", [
+    (8, 2, 2, 64, [2, 50, 3], 64), (4, 1, 20, 128, [2, 100, 1], 100), (8, 2, 2, 256, [2, 2000, 3], None), (4, 1, 3, 64, [2, 1500, 40], 4096),
+    (8, 4, 2, 128, [2, 600] * 32, 600)])
+def test_a_token_that_sees_nothing_is_zero_whatever_its_query(cq, torch, bits, heads, group, dim, lengths, max_length, value):
+    S, page = 4, 16
+    cache = make_cache(torch, cq, bits, sum(-(-n // page) for n in lengths) + 300, heads, page, dim, seed=40)
+    table, lens = make_table(torch, cache, lengths, seed=40, extra=260)
+    Q = queries(torch, len(lengths), S, heads * group, dim, "float16")
+    want = cq.crossquant_cache_attention(cache, Q, table, lens, max_length=max_length)
+    blind = torch.arange(S, device="cuda") < S - lens[:, None]
+    assert blind[0].tolist() == [True, True, False, False]
+    Q[:, :, ::2, 5] = value
+    out = cq.crossquant_cache_attention(cache, Q, table, lens, max_length=max_length)
+    assert (out[blind] == 0).all()
+    assert torch.isnan(out[~blind][:, ::2]).all()
+    assert torch.equal(out[:, :, 1::2], want[:, :, 1::2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("length", [50, 1500])
+def test_a_token_whose_pages_do_not_exist_is_zero_whatever_its_query(cq, torch, length, value):
+    cache = make_cache(torch, cq, 8, 10, 2, 16, 64, seed=8)
+    table = torch.full((1, length // 16 + 1), -1, dtype=torch.int32, device="cuda")
+    table[0, 1::2] = 10
+    lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+    Q = queries(torch, 1, 2, 4, 64, "float16")
+    Q[0, 1, 1, 7] = value
+    assert (cq.crossquant_cache_attention(cache, Q, table, lens) == 0).all()
+    table[0, 1] = 3
+    out = cq.crossquant_cache_attention(cache, Q, table, lens)
+    assert torch.isnan(out[0, 1, 1]).all()
+    out[0, 1, 1] = 0.0
+    assert torch.isfinite(out).all()
