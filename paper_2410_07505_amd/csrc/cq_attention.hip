@@ -414,8 +414,9 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
                     const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r + 1], row_factor[mr], -ref));
                     l[mr] += e0 + e1;
                     v2f w = {e0 * v.a[t][r], e1 * v.a[t][r + 1]};
-                    // (of two rows one may see a position whose scale is no number, and the other not)
-                    if (MR > 1 && masked) w = v2f{e0 == 0.0f ? 0.0f : w[0], e1 == 0.0f ? 0.0f : w[1]};
+                    // (of two rows one may see a position whose scale is no number, and the other not: by the score, as a weight that
+                    // is 0 in binary32 does not hide it)
+                    if (MR > 1 && masked) w = v2f{z[mr][t][r] == -INFINITY ? 0.0f : w[0], z[mr][t][r + 1] == -INFINITY ? 0.0f : w[1]};
                     const v2h w16 = __builtin_convertvector(w, v2h);
                     const v2f rest = {__builtin_fmaf((float)w16[0], -1.0f, w[0]), __builtin_fmaf((float)w16[1], -1.0f, w[1])};
                     const v2h rest16 = __builtin_convertvector(rest, v2h);

@@ -63,6 +63,30 @@ def test_an_infinite_key_or_value_shows(cq, torch, side, form, bits, kind, value
     assert torch.equal(out, want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [4, 20])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("n", [20, 40, 700])
+def test_a_value_with_no_number_shows_at_any_weight(cq, torch, n, bits, group):
+    """A visible position whose softmax weight is 0 in binary32 and whose value is no number: zero times that is none either, in the
+    sequence's last tile as in those before it.  An earlier token, which does not see it, is free of it."""
+    cache = make_cache(torch, cq, bits, n // 16 + 1, 1, 16, 64, cols=False, seed=41)
+    table, lens = make_table(torch, cache, [n], seed=41, extra=0)
+    Q = torch.zeros((1, 2, group, 64), dtype=torch.float16, device="cuda")
+    Q[..., 0] = 1.0
+    cache.k_codes.zero_()
+    cache.k_scale.fill_(1.0)
+    for pos in (0, n - 2, n - 1):
+        page, place = int(table[0, pos // 16]), pos % 16
+        cache.k_codes[page, 0, place, 0] = -7 if bits == 8 else 9
+        kept = cache.v_scale[page, 0, place].clone()
+        cache.v_scale[page, 0, place] = float("nan")
+        out = cq.crossquant_cache_attention(cache, Q, table, lens, scale=100.0)
+        assert torch.isnan(out[0, 1]).all()
+        assert torch.isfinite(out[0, 0]).all() if pos == n - 1 else torch.isnan(out[0, 0]).all()
+        cache.v_scale[page, 0, place] = kept
+
+
 # ---- tokens that see nothing ---------------------------------------------------------------------------------------
 
 @pytest.mark.gpu
