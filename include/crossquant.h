@@ -388,8 +388,8 @@ int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T
  * workspace: crossquant_cache_attention_workspace(...) bytes, 16-byte aligned (0 bytes: may be NULL), for this call alone until it is done: calls that
  *   may overlap, and graphs that may, take one each.  Need not be cleared.
  * Queries enter the product as 16-bit fixed-point numbers relative to their row's largest |q_j b_j| (at most 1.6e-5 of it off), codes as they
- * are; scores, softmax statistics and sums are binary32, the weights of the values two binary16 numbers each (22 bits), relative to the
- * largest.
+ * are; scores, softmax statistics and sums are binary32.  The weights of the values, softmax weight times the value row's factor, are two
+ * binary16 numbers each: 22 bits down to 2^-16 of the row's largest product of the two, and never off by more than 2^-38 of that.
  */
 int64_t crossquant_cache_attention_workspace(const cq_cache *cache, int64_t B, int64_t S, int64_t q_heads, int64_t max_length);
 int crossquant_cache_attention(const cq_cache *cache, const void *Q, int64_t q_batch_stride, int64_t q_token_stride,

@@ -13,9 +13,12 @@
 // operand is q' as 16-bit fixed-point number relative to the row's largest |q'|: two signed digits, two products, an exact 32-bit
 // sum (256 high + low: at most 256 * 127 * 32512 < 2^31), off by at most 1.6e-5 (half of 1 / 32512) of that largest.  Against codes turned into
 // binary16: no conversion of K at all, at the same matrix time.  INT4 codes enter as 16 times their value (a mask or a shift).
-// Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) relative to the largest a so
-// far (a power of two R, 2^14 / R; the sums are rescaled when R grows, as for m), which leaves 38 binades below the largest weight;
-// codes become binary16 exactly (as subnormal numbers, and from there in one fused step).  With one number a weight the result was off by sqrt(2) times what its
+// Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) in units of 2^-14 R, R the row's
+// largest w so far up to a power of two.  R shrinks with the weights as m grows, so that the sums, in units of it too, need no
+// rescaling then; a larger w takes a new R and rescales them.  The 22 bits reach 16 binades below the largest w, the units of the second
+// number 38.  (With R from the largest a, whatever its position's score, as here before, a value 2^30 times the others that no query
+// attends to took all but 8 bits of them: 64 x 1024-8192 125.3 us now and 124.4 then, 2 x 131072 INT4 62.7 and 61.)
+// Codes become binary16 exactly (as subnormal numbers, and from there in one fused step).  With one number a weight the result was off by sqrt(2) times what its
 // own rounding to binary16 costs; the second product is in the shadow of the loads.  Sums, m and the sum of 2^(z - m) are binary32.
 //
 // No operand passes through LDS.  The score tile is keys x rows, so that a lane holds scores of one row (lane & 15) for the positions
@@ -38,7 +41,7 @@ constexpr int kSub = 2;                                    // subtiles of 16 pos
 constexpr int kTile = 16 * kSub, kBlockStep = kWaves * kTile;
 constexpr float kDigits = 32512.0f;                        // 127 * 256
 constexpr float kWeightTop = 16384.0f;                     // 2^14
-constexpr float kSmallest = 7.888609052210118e-31f;        // 2^-100: queries and scales below count as zero
+constexpr float kSmallest = 7.888609052210118e-31f;        // 2^-100: queries below count as zero, and R is no smaller
 
 struct Args {
     const uint16_t* Q;
@@ -299,7 +302,9 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
     for (int mr = 0; mr < MR; ++mr)
 #pragma unroll
         for (int i = 0; i < kOut; ++i) o[mr][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    float R = kSmallest, to_weight = kWeightTop / kSmallest;      // the power of two above every a of V so far (from 2^-100)
+    float R[MR];                                           // above every product 2^(z - m) a of the row so far; o is in units of it
+#pragma unroll
+    for (int mr = 0; mr < MR; ++mr) R[mr] = 0.0f;
     // codes leave the subnormal numbers times 2^10 and without what was added to them: q 2^-14
     const v2h code_unit = (v2h)(_Float16)1024.0f, code_zero = (v2h)(_Float16)(BITS == 8 ? -0.0078125f : -0.00048828125f);
 
@@ -366,25 +371,6 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             if ((++tile & 31) == 0) load_pages(next);
             load_keys(k, next, tile);
         }
-        // the scale of the weights: a power of two above every a so far
-        float va_top = 0.0f;
-#pragma unroll
-        for (int t = 0; t < kSub; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) va_top = fmaxf(va_top, v.a[t][r]);
-        float shrink = 1.0f;
-        if (__any(va_top >= R)) {                          // seldom after the first tile
-            va_top = max_groups(va_top);
-            const float R_new = fmaxf(R, __uint_as_float((__float_as_uint(va_top) & 0x7F800000u) + 0x00800000u));
-            shrink = R / R_new;
-            R = R_new;
-            to_weight = kWeightTop / R_new;
-        }
-#pragma unroll
-        for (int t = 0; t < kSub; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v.a[t][r] *= to_weight;
-
         v8h p[MR][kSub / 2], p_rest[MR][kSub / 2];
 #pragma unroll
         for (int mr = 0; mr < MR; ++mr) {
@@ -398,27 +384,46 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             const float keep = __builtin_amdgcn_exp2f(m[mr] - ref);
             m[mr] = top;
             l[mr] *= keep;
-            const float factor = keep * shrink;
-            if (__any(factor != 1.0f)) {
+            float w[kSub][4], w_top = 0.0f;
+#pragma unroll
+            for (int t = 0; t < kSub; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r], row_factor[mr], -ref));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r + 1], row_factor[mr], -ref));
+                    l[mr] += e0 + e1;
+                    w[t][r] = e0 * v.a[t][r];
+                    w[t][r + 1] = e1 * v.a[t][r + 1];
+                    // (of two rows one may see a position whose scale is no number, and the other not: by the score, as a weight that
+                    // is 0 in binary32 does not hide it)
+                    if (MR > 1 && masked) {
+                        if (z[mr][t][r] == -INFINITY) w[t][r] = 0.0f;
+                        if (z[mr][t][r + 1] == -INFINITY) w[t][r + 1] = 0.0f;
+                    }
+                    w_top = fmaxf(w_top, fmaxf(w[t][r], w[t][r + 1]));
+                }
+            // Sums so far shrink with R as m grows; a larger product, or an R about to leave the normal numbers, takes a new power of two.
+            R[mr] *= keep;
+            if (__any((w_top >= R[mr]) | (R[mr] < kSmallest))) {
+                w_top = max_groups(w_top);
+                const bool more = (w_top >= R[mr]) | (R[mr] < kSmallest);
+                const float R_new = more ? fmaxf(kSmallest, __uint_as_float((__float_as_uint(w_top) & 0x7F800000u) + 0x00800000u)) : R[mr];
+                const float shrink = R[mr] / R_new;
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[mr][i][r] *= factor;
+                    for (int r = 0; r < 4; ++r) o[mr][i][r] *= shrink;
+                R[mr] = R_new;
             }
+            const float to_weight = kWeightTop * __builtin_amdgcn_rcpf(R[mr]);
 #pragma unroll
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
                     typedef float v2f __attribute__((ext_vector_type(2)));
-                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r], row_factor[mr], -ref));
-                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r + 1], row_factor[mr], -ref));
-                    l[mr] += e0 + e1;
-                    v2f w = {e0 * v.a[t][r], e1 * v.a[t][r + 1]};
-                    // (of two rows one may see a position whose scale is no number, and the other not: by the score, as a weight that
-                    // is 0 in binary32 does not hide it)
-                    if (MR > 1 && masked) w = v2f{z[mr][t][r] == -INFINITY ? 0.0f : w[0], z[mr][t][r + 1] == -INFINITY ? 0.0f : w[1]};
-                    const v2h w16 = __builtin_convertvector(w, v2h);
-                    const v2f rest = {__builtin_fmaf((float)w16[0], -1.0f, w[0]), __builtin_fmaf((float)w16[1], -1.0f, w[1])};
+                    const v2f u = {w[t][r] * to_weight, w[t][r + 1] * to_weight};
+                    const v2h w16 = __builtin_convertvector(u, v2h);
+                    const v2f rest = {__builtin_fmaf((float)w16[0], -1.0f, u[0]), __builtin_fmaf((float)w16[1], -1.0f, u[1])};
                     const v2h rest16 = __builtin_convertvector(rest, v2h);
                     const int at = 4 * (t & 1) + r;
                     p[mr][t / 2][at] = w16[0];
@@ -463,7 +468,6 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
     }
 
     // ---- the waves' results meet: 16 rows at a time
-    const float unit = R;                                  // of 2^14 / R a weight and 2^-14 a code
 #pragma unroll
     for (int mr = 0; mr < MR; ++mr) {
         __syncthreads();                                   // (what the last piece or rows left has been read)
@@ -478,7 +482,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
 #pragma unroll
             for (int i = 0; i < kOut; i += 4)
                 *reinterpret_cast<float4*>(&sh.o[wave][fr][kOut * (4 * grp + r) + i]) =
-                    make_float4(o[mr][i][r] * unit, o[mr][i + 1][r] * unit, o[mr][i + 2][r] * unit, o[mr][i + 3][r] * unit);
+                    make_float4(o[mr][i][r] * R[mr], o[mr][i + 1][r] * R[mr], o[mr][i + 2][r] * R[mr], o[mr][i + 3][r] * R[mr]);
         __syncthreads();
         constexpr int kCols = DIM / 16;                    // channels a thread joins
         const int row = threadIdx.x / 16, d0 = threadIdx.x % 16 * kCols, in_tile = 16 * mr + row;

@@ -1,9 +1,12 @@
-"""The quantized cache where single numbers decide: rows that hold no number, tokens that see nothing."""
+"""The quantized cache where single numbers decide: rows that hold no number, tokens that see nothing, values whose scales
+lie far apart."""
 from __future__ import annotations
+
+import math
 
 import pytest
 
-from test_cache import cq, make_cache, make_table, queries, torch  # noqa: F401 (fixtures)
+from test_cache import ROUND, attention_oracle, cq, make_cache, make_table, places, queries, torch  # noqa: F401 (fixtures)
 
 
 # ---- rows that hold no number --------------------------------------------------------------------------------------
@@ -125,3 +128,165 @@ def test_a_token_whose_pages_do_not_exist_is_zero_whatever_its_query(cq, torch, 
     assert torch.isnan(out[0, 1, 1]).all()
     out[0, 1, 1] = 0.0
     assert torch.isfinite(out).all()
+
+
+# ---- weights -------------------------------------------------------------------------------------------------------
+
+def weight_tolerance(torch, cache, Q, table, lengths, scale, max_length, ref):
+    """How far a result may be off where no digit of a query is lost, before its own rounding.
+
+    A score z passes seven roundings to binary32 (the integer product, the key's factor, three of the row's factor, the product, the
+    exponent), each 2^-24 of it: dz = 2^-21 |z|, in numerator and denominator.  The exponential, its product with the value's factor and
+    the weights' common factor (reciprocal included) are 6 times 2^-23; the two numbers of a weight keep it to 2^-22 of itself, and to
+    2^-25 of the unit 2^-14 R where they are subnormal, R at most twice the largest product of a softmax weight and a factor of the
+    row.  Sums are binary32: a rounding (counted twice: the matrix instruction may truncate) for each value that is not zero, the
+    8 waves, the pieces, and the factors that join them."""
+    B, S, HQ, D = Q.shape
+    H, page, q_max = cache.heads, cache.page_size, 127 if cache.bits == 8 else 7
+    ck, ak, bk = places(torch, cache, "k")
+    cv, av, bv = places(torch, cache, "v")
+    tol = torch.zeros_like(ref)
+    for b in range(B):
+        for s in range(S):
+            m = max(0, min(int(lengths[b]) - (S - 1 - s), max_length))
+            pos = torch.arange(m, device=Q.device)
+            at = table[b].long()[pos // page] * page + pos % page
+            if m == 0:
+                continue
+            for h in range(H):
+                g = slice(h * (HQ // H), (h + 1) * (HQ // H))
+                z = scale * ((Q[b, s, g].double() * bk[h]) @ (ck[at, h] * ak[at, h, None]).t())
+                p = torch.softmax(z, -1)
+                size = p @ (cv[at, h] * av[at, h, None]).abs()
+                terms = (cv[at, h] != 0).sum(0)                              # of each channel
+                most = (p * av[at, h]).amax(-1, keepdim=True)
+                dz = 2.0 ** -21 * z.abs().amax(-1, keepdim=True)
+                tol[b, s, g] = bv[h] * ((torch.expm1(2 * dz) + 6 * 2.0 ** -23 + 2.0 ** -22 + (2 * terms + 64) * 2.0 ** -24) * size
+                                        + m * 2.0 ** -38 * q_max * most)
+    return tol
+
+
+def check_weights(torch, cq, cache, Q, table, lengths, scale=None, max_length=None):
+    scale = cache.dim ** -0.5 if scale is None else scale
+    most = table.shape[1] * cache.page_size if max_length is None else max_length
+    out = cq.crossquant_cache_attention(cache, Q, table, lengths, scale=scale, max_length=max_length)
+    ref, _ = attention_oracle(torch, cache, Q, table, lengths, scale, most)
+    tol = weight_tolerance(torch, cache, Q, table, lengths, scale, most, ref)
+    kind = str(Q.dtype).split(".")[1]
+    bad = ~((out.double() - ref).abs() <= ROUND[kind] * ref.abs() + (1 + ROUND[kind]) * tol + (2.0 ** -25 if kind == "float16" else 0.0))
+    assert not bad.any(), "%d of %d outputs, the first at %s: %s, not %s" % (
+        int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist(), out[bad][0].item(), ref[bad][0].item())
+
+
+def set_values(torch, cache, codes, scale, at):
+    """Values and their factors of the places `at`, from [place][head][dim] and [place][head]."""
+    page = cache.page_size
+    c = codes.to(torch.int64) & 15
+    c = codes.to(torch.int8) if cache.bits == 8 else (c[..., 0::2] | (c[..., 1::2] << 4)).to(torch.uint8)
+    cache.v_codes[at // page, :, at % page] = c.to(cache.v_codes.device)
+    cache.v_scale[at // page, :, at % page] = scale.to(cache.v_scale)
+
+
+def cancelling_values(torch, n, heads, dim, q_max, seed):
+    """Values of n positions, 16 of which are not zero: pairs of opposite codes whose factors differ by some per cent, so that sums are
+    a few hundredths of their terms and a weight's own rounding shows in them."""
+    g = torch.Generator().manual_seed(seed)
+    codes, scale = torch.zeros((n, heads, dim)), torch.ones((n, heads))
+    at = torch.randperm(n, generator=g)[:16]
+    half = torch.randint(1, q_max + 1, (8, heads, dim), generator=g) * (2 * torch.randint(0, 2, (8, heads, dim), generator=g) - 1)
+    codes[at[:8]], codes[at[8:]] = half.float(), -half.float()
+    first = 0.01 * (1.0 + torch.rand((8, heads), generator=g))
+    scale[at[:8]], scale[at[8:]] = first, first * (1.0 + 0.05 * torch.rand((8, heads), generator=g))
+    return codes, scale
+
+
+FLAT = [(40, 2, 4, 1, 64, 16, 64), (300, 2, 20, 1, 128, 16, 400), (500, 1, 4, 2, 256, 32, None), (1500, 2, 3, 1, 128, 64, None), (1400, 1, 20, 1, 64, 32, 2000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("form", range(len(FLAT)))
+def test_weights_keep_their_bits(cq, torch, form, bits, kind):
+    """scale 0: every score is exactly 0, and sums that cancel show the weights' own rounding (one binary16 number a weight is off by
+    some 20 times the tolerance, see the test of the two forms on the CPU)."""
+    n, heads, group, S, dim, page, max_length = FLAT[form]
+    cache = make_cache(torch, cq, bits, n // page + 1, heads, page, dim, cols=False, seed=form)
+    table, lens = make_table(torch, cache, [n], seed=form, extra=30)
+    pos = torch.arange(n)
+    at = (table[0].cpu().long()[pos // page] * page + pos % page).cuda()
+    set_values(torch, cache, *cancelling_values(torch, n, heads, dim, 127 if bits == 8 else 7, form), at)
+    check_weights(torch, cq, cache, queries(torch, 1, S, heads * group, dim, kind), table, lens, scale=0.0, max_length=max_length)
+
+
+def test_one_number_a_weight_is_not_enough(torch):
+    """On the CPU: the weights of the test above as two binary16 numbers stay within its tolerance, as one they do not."""
+    n, dim = 40, 64
+    codes, scale = cancelling_values(torch, n, 1, dim, 127, 0)
+    codes, a = codes[:, 0].double(), scale[:, 0].double()
+    R = 2.0 ** math.ceil(math.log2(float(a.max())) + 1e-9)
+    w = a * 2.0 ** 14 / R
+    first = w.half().double()
+    both = first + (w - first).half().double()
+    exact, size = (w @ codes), (w @ codes.abs())
+    terms = (codes != 0).sum(0)
+    tol = ROUND["float16"] * exact.abs() + (6 * 2.0 ** -23 + 2.0 ** -22 + (2 * terms + 64) * 2.0 ** -24) * size
+    assert ((both @ codes - exact).abs() <= 2.0 ** -22 * size).all()
+    off = (first @ codes - exact).abs() / tol
+    assert off.max() > 2 and (off > 1).sum() > dim // 8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("binades", [20, 33, 45, 80])
+@pytest.mark.parametrize("bits,n,heads,group,S,dim,page,max_length,kind", [
+    (8, 30, 2, 2, 1, 64, 16, 64, "float16"), (4, 300, 1, 20, 2, 128, 16, 400, "bfloat16"), (8, 400, 1, 4, 1, 256, 32, None, "float16"),
+    (8, 1500, 2, 4, 1, 128, 64, None, "bfloat16"), (4, 1400, 1, 20, 1, 64, 32, 2000, "float16")])
+def test_a_value_that_no_weight_asks_for_takes_no_bits(cq, torch, bits, n, heads, group, S, dim, page, max_length, kind, binades):
+    """Positions with enormous values and a softmax weight of 2^-101 beside others of ordinary values: results are the others'.  Early
+    and late ones, in one tile with the others and in tiles of their own; every second query has the opposite sign, and the enormous
+    values are all that it attends to."""
+    cache = make_cache(torch, cq, bits, n // page + 1, heads, page, dim, cols=False, seed=51)
+    table, lens = make_table(torch, cache, [n], seed=51, extra=30)
+    q_max = 127 if bits == 8 else 7
+    g = torch.Generator().manual_seed(n + binades)
+    big = torch.zeros(n, dtype=torch.bool)
+    big[torch.randperm(n, generator=g)[:3]] = True
+    big[n // 2:n // 2 + 40] = True
+    big[[0, n - 1]] = True
+    pos = torch.arange(n)
+    at = (table[0].cpu().long()[pos // page] * page + pos % page).cuda()
+    cache.k_codes.zero_()
+    cache.k_scale.fill_(1.0)
+    sign = torch.where(big, -q_max, q_max)
+    cache.k_codes[at // page, :, at % page, 0] = (sign if bits == 8 else sign & 15).to(cache.k_codes)[:, None]
+    scale = 0.01 * torch.exp(0.3 * torch.randn((n, heads), generator=g)) * torch.where(big, 2.0 ** binades, 1.0)[:, None]
+    set_values(torch, cache, torch.randint(-q_max, q_max + 1, (n, heads, dim), generator=g).float(), scale, at)
+    Q = torch.zeros((1, S, heads * group, dim), dtype=getattr(torch, kind), device="cuda")
+    Q[..., 0] = 1.0
+    Q[:, :, 1::2, 0] = -1.0
+    if kind == "float16":
+        Q[:, :, 1::2, 0] = 1.0                                               # (no binary16 result of that size)
+    check_weights(torch, cq, cache, Q, table, lens, scale=35.0 / q_max, max_length=max_length)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("binades", [20, 45, 80])
+@pytest.mark.parametrize("n", [100, 400, 3000])
+def test_weights_that_later_scores_outweigh(cq, torch, n, binades):
+    """Scores rise along the sequence, in small steps and in one large one, while the values' factors fall: what was the largest
+    product at first is nothing at the end."""
+    cache = make_cache(torch, cq, 8, n // 16 + 1, 1, 16, 64, cols=False, seed=52)
+    table, lens = make_table(torch, cache, [n], seed=52)
+    pos = torch.arange(n)
+    at = (table[0].cpu().long()[pos // 16] * 16 + pos % 16).cuda()
+    g = torch.Generator().manual_seed(n)
+    cache.k_codes.zero_()
+    cache.k_scale.fill_(1.0)
+    for steps in (127, 1):
+        rise = torch.div(pos * steps, n - 1, rounding_mode="floor") * (254 // steps) - 127
+        cache.k_codes[at // 16, :, at % 16, 0] = rise.to(cache.k_codes)[:, None]
+        scale = 0.01 * torch.exp2(-binades * (rise + 127) / 254.0)[:, None] * (1.0 + torch.rand((n, 1), generator=g)) * 2.0 ** binades
+        set_values(torch, cache, torch.randint(-127, 128, (n, 1, 64), generator=g).float(), scale, at)
+        Q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+        Q[..., 0] = torch.tensor([1.0, 0.5])
+        check_weights(torch, cq, cache, Q, table, lens, scale=80.0 / 254.0)
