@@ -383,7 +383,7 @@ int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T
  * codes and scales there.  A query that holds an infinity or NaN makes its row NaN.
  * Q, out: type `type`; Q: token s of sequence b at b * q_batch_stride + s * q_token_stride, head h another h * q_head_stride
  *   elements on (16-byte aligned, strides multiples of 8, else CQ_ERR_ALIGN); out: [B][S][q_heads][dim], contiguous, 16-byte aligned.
- * q_heads: a multiple of the cache's heads.  page_table: int32 [B][table_width]; lengths: int32 [B].
+ * q_heads: a multiple of the cache's heads; B * S * q_heads below 2^27.  page_table: int32 [B][table_width]; lengths: int32 [B].
  * max_length: no visible position is at or past it (1 .. table_width * page_size, at most 2^31 - 256): what a launch is sized for.
  * workspace: crossquant_cache_attention_workspace(...) bytes, 16-byte aligned (0 bytes: may be NULL), for this call alone until it is done: calls that
  *   may overlap, and graphs that may, take one each.  Need not be cleared.

@@ -89,7 +89,7 @@ int check_row_stride(int64_t stride) {
 // B, S, q_heads and max_length of an attention call
 int check_attention(const cq::CacheView& c, int64_t B, int64_t S, int64_t q_heads, int64_t max_length) {
     if (!dim_ok(B) || !dim_ok(S) || !dim_ok(q_heads) || q_heads % c.heads != 0) return CQ_ERR_SHAPE;
-    if (S * q_heads > CQ_MAX_DIM || B * S * q_heads > (int64_t)1 << 31 || B * S * q_heads * c.dim > CQ_MAX_ELEMS) return CQ_ERR_SHAPE;
+    if (S * q_heads > CQ_MAX_DIM || B * S * q_heads >= (int64_t)1 << 27) return CQ_ERR_SHAPE;    // (what one launch can join)
     return max_length >= 1 && max_length <= ((int64_t)1 << 31) - 256 ? CQ_OK : CQ_ERR_SHAPE;     // (positions step past it by 128)
 }
 

@@ -770,7 +770,7 @@ attention_join_kernel(Args a, int rows_per_tile) {
 // - four units: one sequence (8 pairs) of 256 (500) positions 8.4 (10.5) us so, 11.6 (11.7) in stretches, 640 positions 11.4 and 11.8;
 // - sixteen where they keep half the CUs busy: of up to 1024 positions, 100 sequences 31 and 40, 200 67 and 77; of up to 2048, 60
 //   37 and 40, 100 62 and 68, 400 211 and 224;
-// - what each of the chip's places gets of them where that is more still.
+// - what each of the chip's places gets of them where that is more still (and never for 2^24 pairs and more, which no launch holds).
 // Pairs of more than four units that do not fill the CUs twice have blocks of eight waves, half the steps: 16 sequences of up to 1024
 // (2048) positions 14.9 (21.3) us, with four waves 16.9, in stretches 18.8 (24.2); 30: 15.9 (22.7), 17.5, (29.4).  With four units the
 // longer way to one result costs as much: 10.7 and 10.5; with more pairs eight waves are in each other's way: 48 of 1024 24.6 and 21.3.
@@ -789,7 +789,7 @@ Plan plan(const CacheView& c, const AttentionShape& s) {
     p.pairs = s.B * c.heads * p.row_tiles;
     p.n_blocks = p.mr > 1 || c.dim == 256 ? 512 : c.dim == 128 ? 768 : 1024;
     const int64_t longest = (s.max_length + (int64_t)kBlockStep - 1) / kBlockStep;
-    if (longest <= (p.pairs < 128 ? 4 : std::max<int64_t>(16, p.pairs / p.n_blocks))) p.n_blocks = 0;
+    if (grid_fits(p.pairs, 64 * kWaves) && longest <= (p.pairs < 128 ? 4 : std::max<int64_t>(16, p.pairs / p.n_blocks))) p.n_blocks = 0;
     p.wide = p.n_blocks == 0 && longest > 4 && p.pairs <= 256;
     return p;
 }
@@ -809,8 +809,8 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
                                   float scale, uint16_t* out, float* workspace, hipStream_t stream) {
     const Plan p = plan(c, s);
     const int group = s.q_heads / c.heads;
-    const int64_t blocks = p.n_blocks ? p.n_blocks : p.pairs, rows = s.B * c.heads * s.S * group;
-    if (!grid_fits(blocks, 64 * kWaves) || !grid_fits(rows, 256)) return hipErrorInvalidValue;
+    const int64_t blocks = p.n_blocks ? p.n_blocks : p.pairs, rows = s.B * c.heads * s.S * group, join_blocks = rows >= 1024 ? (rows + 7) / 8 : rows;
+    if (!grid_fits(blocks, p.wide ? 64 * 8 : 64 * kWaves) || (p.n_blocks && !grid_fits(join_blocks, 256))) return hipErrorInvalidValue;
     Args a;
     a.Q = Q; a.q_batch = q_batch; a.q_token = q_token; a.q_head = q_head;
     a.k_codes = c.k_codes; a.v_codes = c.v_codes; a.k_scale = c.k_scale; a.v_scale = c.v_scale; a.k_col = c.k_col; a.v_col = c.v_col;
@@ -841,8 +841,8 @@ hipError_t launch_cache_attention(const CacheView& c, const AttentionShape& s, c
     else with_bits(std::integral_constant<int, 4>());
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_blocks == 0) return e;
     auto join = [&](auto many, auto few) {
-        if (rows >= 1024) many<<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(a, 16 * p.mr, rows);
-        else few<<<(unsigned)rows, 256, 0, stream>>>(a, 16 * p.mr);
+        if (rows >= 1024) many<<<(unsigned)join_blocks, 256, 0, stream>>>(a, 16 * p.mr, rows);
+        else few<<<(unsigned)join_blocks, 256, 0, stream>>>(a, 16 * p.mr);
     };
     if (c.dim == 64) join(attention_join_rows_kernel<64>, attention_join_kernel<64>);
     else if (c.dim == 128) join(attention_join_rows_kernel<128>, attention_join_kernel<128>);

@@ -1,12 +1,14 @@
 """The quantized cache where single numbers decide: rows that hold no number, tokens that see nothing, values whose scales
-lie far apart."""
+lie far apart, and the largest calls."""
 from __future__ import annotations
 
 import math
 
 import pytest
 
-from test_cache import ROUND, attention_oracle, cq, make_cache, make_table, places, queries, torch  # noqa: F401 (fixtures)
+from test_cache import ROUND, attention_oracle, cq, descriptor, make_cache, make_table, places, queries, torch  # noqa: F401 (fixtures)
+
+P = 0x10000
 
 
 # ---- rows that hold no number --------------------------------------------------------------------------------------
@@ -290,3 +292,38 @@ def test_weights_that_later_scores_outweigh(cq, torch, n, binades):
         Q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
         Q[..., 0] = torch.tensor([1.0, 0.5])
         check_weights(torch, cq, cache, Q, table, lens, scale=80.0 / 254.0)
+
+
+# ---- the largest calls ---------------------------------------------------------------------------------------------
+
+def test_size_limits_are_the_same_for_workspace_and_call(cq):
+    c = descriptor(cq, heads=1)
+
+    def both(B, S, HQ, most=64, width=4):
+        need = cq.raw.crossquant_cache_attention_workspace(c, B, S, HQ, most)
+        status = cq.raw.crossquant_cache_attention(c, P, 64, 64, 64, 0, B, S, HQ, P, width, P, most, 0.1, P, P, need - 1, None)
+        return need, status
+    for B, S, HQ in ((1 << 24, 8, 1), (2048, 1024, 64), (1 << 24, 128, 1)):
+        assert both(B, S, HQ) == (-1, -2)
+    for B, S, HQ in ((64, 4096, 64), (1 << 24, 1, 1), (1 << 24, 7, 1), (2047, 1024, 64)):
+        need, status = both(B, S, HQ, 1 << 20, 1 << 16)
+        assert need > 0 and status == -2                                     # (a byte too few)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,S,heads,group,max_length", [(64, 4096, 1, 64, 64), (64, 4096, 1, 64, 1 << 18), ((1 << 20) + 3, 1, 16, 1, 64)])
+def test_calls_of_more_than_sixteen_million_rows(cq, torch, B, S, heads, group, max_length):
+    """One query row for all, so that a few small calls say what each row is."""
+    dim, page = 64, 65536 if max_length > 64 else 16
+    cache = make_cache(torch, cq, 8, 4, heads, page, dim, seed=70)
+    width = -(-max_length // page)
+    table = torch.arange(width, dtype=torch.int32, device="cuda").expand(B, width).contiguous()
+    lens = (torch.arange(B, device="cuda") % 61).to(torch.int32)
+    one = queries(torch, 1, 1, heads * group, dim, "bfloat16")
+    out = cq.crossquant_cache_attention(cache, one.expand(B, S, -1, -1), table, lens, max_length=max_length)
+    few = torch.arange(61, dtype=torch.int32, device="cuda")
+    want = cq.crossquant_cache_attention(cache, one.expand(61, 1, -1, -1), table[:61].contiguous(), few, max_length=64)[:, 0]
+    size = -(-B // 8)
+    for b in range(0, B, size):
+        seen = (lens[b:b + size, None] - (S - 1 - torch.arange(S, device="cuda"))).clamp(min=0)
+        assert torch.equal(out[b:b + size].view(torch.int16), want[seen].view(torch.int16))
