@@ -586,10 +586,11 @@ hipError_t launch_fp8_linear(const void* qx, const float* x_scale, const void* q
         }
     }
     // Weights that one row of tiles reads once and that no cache keeps are requested non-temporally: 16 x 8192 x 28672 45.4 -> 41.5 us,
-    // 128 x 8192 x 28672 66.3 -> 61.9; three weights of 64 MiB in turn, which the memory-side cache holds, 12.6 -> 15.1.
+    // 128 x 8192 x 28672 66.3 -> 61.9, 1 x 65536 x 4096 56 -> 50, 8 x 53248 x 4096 49 -> 46; three weights of 64 MiB in turn, which the
+    // memory-side cache holds, 12.6 -> 15.1.
     const bool once = form >= 0 && T <= kForms[form].tm && (int64_t)I * O > (int64_t)128 << 20;
     switch (form) {
-        case 0: return go<1, 1, 1, 1, 8, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
+        case 0: return once ? go<1, 1, 1, 1, 8, 4, true>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream) : go<1, 1, 1, 1, 8, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
         case 1: return once ? go<1, 1, 1, 2, 4, 3, true>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream) : go<1, 1, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
         case 2: return once ? go<2, 1, 1, 2, 4, 4, true>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream) : go<2, 1, 1, 2, 4, 4>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);
         case 3: return once ? go<2, 2, 1, 2, 4, 3, true>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream) : go<2, 2, 1, 2, 4, 3>(x, x_scale, w, w_scale, T, nk, O, Y, bf16, ldy, stream);

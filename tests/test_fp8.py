@@ -231,6 +231,13 @@ def test_linear_with_large_weights(cq, torch, T, I, O, kind):
     test_linear(cq, torch, T, I, O, kind)
 
 
+# the same by the tiles that the shapes above leave out: 16 x 16
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,I,O,kind", [(8, 53248, 2600, "float16"), (1, 65536, 2100, "bfloat16")])
+def test_linear_with_large_weights_by_the_smallest_tiles(cq, torch, T, I, O, kind):
+    test_linear(cq, torch, T, I, O, kind)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("offset,pitch", [(0, 336), (0, 300), (4, 304), (1, 301), (2, 310)])
 @pytest.mark.parametrize("T", [5, 70, 260])
