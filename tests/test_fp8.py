@@ -238,6 +238,14 @@ def test_linear_with_large_weights_by_the_smallest_tiles(cq, torch, T, I, O, kin
     test_linear(cq, torch, T, I, O, kind)
 
 
+# by 32 x 32 and 64 x 64 tiles (the rows of the list further up whose contraction is 131200 take 16 x 16 ones, and 32 x 32 without
+# the non-temporal form)
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,I,O,kind", [(27, 16512, 8192, "float16"), (32, 59776, 2260, "bfloat16"), (60, 11008, 12300, "float16"), (64, 8320, 16200, "bfloat16")])
+def test_linear_with_large_weights_by_middle_tiles(cq, torch, T, I, O, kind):
+    test_linear(cq, torch, T, I, O, kind)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("offset,pitch", [(0, 336), (0, 300), (4, 304), (1, 301), (2, 310)])
 @pytest.mark.parametrize("T", [5, 70, 260])
