@@ -1,5 +1,5 @@
 """The quantized cache where single numbers decide: rows that hold no number, tokens that see nothing, values whose scales
-lie far apart, and the largest calls."""
+lie far apart, queries with a channel far above the others, and the largest calls."""
 from __future__ import annotations
 
 import math
@@ -292,6 +292,32 @@ def test_weights_that_later_scores_outweigh(cq, torch, n, binades):
         Q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
         Q[..., 0] = torch.tensor([1.0, 0.5])
         check_weights(torch, cq, cache, Q, table, lens, scale=80.0 / 254.0)
+
+
+# ---- queries with a channel far above the others -------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("factor", [100.0, 1000.0])
+@pytest.mark.parametrize("bits,n,heads,group,dim,kind", [(8, 300, 2, 4, 128, "float16"), (4, 90, 1, 20, 64, "bfloat16"), (8, 1500, 2, 3, 256, "bfloat16"),
+                                                         (4, 2000, 1, 4, 128, "float16")])
+def test_a_query_with_an_outlying_channel(cq, torch, bits, n, heads, group, dim, kind, factor):
+    """The row's fixed point is relative to the outlier: results are those of the query rounded to it (each element off by at most
+    1.6e-5 of the largest, as documented), with no further loss."""
+    cache = make_cache(torch, cq, bits, n // 16 + 1, heads, 16, dim, seed=61)
+    cache.k_col.fill_(1.0)
+    table, lens = make_table(torch, cache, [n], seed=61)
+    Q = queries(torch, 1, 1, heads * group, dim, kind, 61)
+    Q[..., 9] = factor * (1.0 + Q[..., 9].abs()) * Q[..., 9].sign()
+    x = Q.float()
+    top = x.abs().amax(-1, keepdim=True)
+    fixed = torch.round(x * (torch.full_like(top, 32512.0) / top)).double() * (top.double() / 32512.0)
+    assert ((fixed - x.double()).abs() <= 1.6e-5 * top).all()
+    scale = 1.0 / factor
+    most = table.shape[1] * 16
+    out = cq.crossquant_cache_attention(cache, Q, table, lens, scale=scale)
+    ref, _ = attention_oracle(torch, cache, fixed, table, lens, scale, most)
+    tol = weight_tolerance(torch, cache, fixed, table, lens, scale, most, ref)
+    assert ((out.double() - ref).abs() <= ROUND[kind] * ref.abs() + (1 + ROUND[kind]) * tol + 2.0 ** -25).all()
 
 
 # ---- the largest calls ---------------------------------------------------------------------------------------------
