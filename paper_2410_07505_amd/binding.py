@@ -950,6 +950,13 @@ def _rows(ten, shape, dtype, name: str, like: torch.Tensor):
     return [s if n > 1 else 0 for s, n in zip(ten.stride()[:-1], shape)]
 
 
+def _in_64_bits(*sizes) -> None:
+    """ctypes would hand over such a number's low 64 bits."""
+    for n in sizes:
+        if isinstance(n, int) and not -(1 << 63) <= n < 1 << 63:
+            raise CrossQuantError(-2)
+
+
 def _slots(slots, like: torch.Tensor) -> int:
     if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
         raise TypeError("slots must be a 1-D int32 tensor")
@@ -1011,6 +1018,7 @@ def crossquant_cache_read(cache: CrossQuantCache, slots: torch.Tensor, *, dtype:
 def crossquant_cache_attention_workspace(cache: CrossQuantCache, B: int, S: int, q_heads: int, max_length: int) -> int:
     """Bytes of workspace that crossquant_cache_attention needs for these sizes (0: none)."""
     _cache(cache)
+    _in_64_bits(B, S, q_heads, max_length)
     n = int(lib.crossquant_cache_attention_workspace(cache._struct, B, S, q_heads, max_length))
     if n < 0:
         raise CrossQuantError(-2)
@@ -1047,6 +1055,7 @@ def crossquant_cache_attention(cache: CrossQuantCache, Q: torch.Tensor, page_tab
     _buf(lengths, torch.int32, (B,), "lengths", like)
     if max_length is None:
         max_length = width * cache.page_size
+    _in_64_bits(max_length)
     if out is None:
         out = torch.empty((B, S, q_heads, dim), dtype=Q.dtype, device=like.device)
     else:

@@ -336,6 +336,20 @@ def test_size_limits_are_the_same_for_workspace_and_call(cq):
         assert need > 0 and status == -2                                     # (a byte too few)
 
 
+@pytest.mark.parametrize("size", [(1 << 64) + 64, 1 << 63, -(1 << 64) + 64])
+def test_sizes_past_64_bits_are_refused(cq, torch, size):
+    codes, scale = torch.zeros((4, 2, 16, 64), dtype=torch.int8), torch.zeros((4, 2, 16))
+    cache = cq.crossquant_cache(codes, scale, codes, scale, 8)
+    for sizes in ((size, 1, 2, 64), (1, size, 2, 64), (1, 1, size, 64), (1, 1, 2, size)):
+        with pytest.raises(cq.CrossQuantError) as e:
+            cq.crossquant_cache_attention_workspace(cache, *sizes)
+        assert e.value.status == -2
+    Q, table, lens = torch.zeros((1, 1, 4, 64), dtype=torch.float16), torch.zeros((1, 4), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(cq.CrossQuantError) as e:
+        cq.crossquant_cache_attention(cache, Q, table, lens, max_length=size)
+    assert e.value.status == -2
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("B,S,heads,group,max_length", [(64, 4096, 1, 64, 64), (64, 4096, 1, 64, 1 << 18), ((1 << 20) + 3, 1, 16, 1, 64)])
 def test_calls_of_more_than_sixteen_million_rows(cq, torch, B, S, heads, group, max_length):
