@@ -345,7 +345,6 @@ int crossquant_fp8_linear(const void *qx, const float *x_scale, const void *qw, 
  *   k_codes, v_codes: bits 8: int8 [pages][heads][page_size][dim]; bits 4: packed nibbles [pages][heads][page_size][dim / 2], even
  *     column in the low nibble.  16-byte aligned.  k_scale, v_scale: float [pages][heads][page_size], the rows' factors a.  Who fills a
  *     cache by other means writes factors that are finite and not negative, or NaN for a row that holds no number: not infinite.
- *     Attention takes key factors below 2^96 (bfloat16 keys from 2^98 on can exceed that): with larger ones scores leave binary32.
  *   k_col, v_col: nullable, float [heads][dim], 16-byte aligned: the column factors b.
  *   dim is 64, 128 or 256; page_size a power of two from 16 to 65536 (else CQ_ERR_UNSUPPORTED); pages * page_size < 2^31.
  */
@@ -389,7 +388,8 @@ int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T
  * workspace: crossquant_cache_attention_workspace(...) bytes, 16-byte aligned (0 bytes: may be NULL), for this call alone until it is done: calls that
  *   may overlap, and graphs that may, take one each.  Need not be cleared.
  * Queries enter the product as 16-bit fixed-point numbers relative to their row's largest |q_j b_j| (at most 1.6e-5 of it off: beside a
- *   channel a thousand times the others, those keep 6 bits; a row whose largest is below 2^-100 counts as zero), codes as they are.
+ *   channel a thousand times the others, those keep 6 bits; a row whose largest, or that times |scale|, is below 2^-100 may count as zero), codes
+ *   as they are.
  * Scores, softmax statistics and sums are binary32.  The weights of the values, softmax weight times the value row's factor, are two
  *   binary16 numbers each: 22 bits down to 2^-16 of the row's largest product of the two, and never off by more than 2^-38 of that.
  */

@@ -273,12 +273,11 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             for (int e = 0; e < kRuns * kRun; ++e) x[e] = none ? 0.0f : x[e];
         }
         const bool live = top >= kSmallest && !none;       // kDigits / top stays in range
-        // a score is the digits' product times a factor that is never negative (the digits take the scale's sign) nor zero (which times
-        // the -infinity of an unseen position would be no number)
+        // (the digits take the scale's sign)
         const float inv = live ? (a.scale < 0.0f ? -kDigits : kDigits) / top : 0.0f;
         // (codes of 4 bits enter as 16 times their value)
         const float f = (live ? top / kDigits : 0.0f) * (fabsf(a.scale) * 1.4426950408889634f * (BITS == 4 ? 0.0625f : 1.0f));
-        row_factor[mr] = none ? INFINITY : fmaxf(f, 1.1754943508222875e-38f);
+        row_factor[mr] = none ? INFINITY : f;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -346,8 +345,10 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
                     hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[f], q_hi[mr][f], hi, 0, 0, 0);
                     lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[f], q_lo[mr][f], lo, 0, 0, 0);
                 }
+                // The two factors first: no part leaves binary32 where the score does not.  And rounded before the maximum is taken from it: with
+                // a rounded maximum against products inside a fused step, equal scores of more than 2^32 gave NaN.
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z[mr][t][r] = (float)((hi[r] << 8) + lo[r]) * k.a[t][r];
+                for (int r = 0; r < 4; ++r) z[mr][t][r] = (float)((hi[r] << 8) + lo[r]) * (k.a[t][r] * row_factor[mr]);
             }
         }
         if (masked) {
@@ -379,7 +380,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) top = fmaxf(top, z[mr][t][r]);
-            top = fmaxf(m[mr], max_groups(top) * row_factor[mr]);
+            top = fmaxf(m[mr], max_groups(top));
             const float ref = top == -INFINITY ? 0.0f : top;
             const float keep = __builtin_amdgcn_exp2f(m[mr] - ref);
             m[mr] = top;
@@ -389,8 +390,8 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; r += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r], row_factor[mr], -ref));
-                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mr][t][r + 1], row_factor[mr], -ref));
+                    const float e0 = __builtin_amdgcn_exp2f(z[mr][t][r] - ref);
+                    const float e1 = __builtin_amdgcn_exp2f(z[mr][t][r + 1] - ref);
                     l[mr] += e0 + e1;
                     w[t][r] = e0 * v.a[t][r];
                     w[t][r + 1] = e1 * v.a[t][r + 1];

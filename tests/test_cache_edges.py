@@ -6,7 +6,7 @@ import math
 
 import pytest
 
-from test_cache import ROUND, attention_oracle, cq, descriptor, make_cache, make_table, places, queries, torch  # noqa: F401 (fixtures)
+from test_cache import ROUND, attention_oracle, check_attention, cq, descriptor, make_cache, make_table, places, queries, torch  # noqa: F401 (fixtures)
 
 P = 0x10000
 
@@ -318,6 +318,58 @@ def test_a_query_with_an_outlying_channel(cq, torch, bits, n, heads, group, dim,
     ref, _ = attention_oracle(torch, cache, fixed, table, lens, scale, most)
     tol = weight_tolerance(torch, cache, fixed, table, lens, scale, most, ref)
     assert ((out.double() - ref).abs() <= ROUND[kind] * ref.abs() + (1 + ROUND[kind]) * tol + 2.0 ** -25).all()
+
+
+# ---- scores that are billions ----------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits,n,group,dim,kind,size", [(8, 40, 4, 128, "float16", 6e4), (4, 300, 20, 64, "float16", 6e4), (8, 1500, 4, 256, "float16", 6e4),
+                                                        (4, 100, 3, 128, "bfloat16", 1e9), (8, 700, 20, 128, "bfloat16", 1e9)])
+def test_scores_of_the_types_largest_numbers(cq, torch, bits, n, group, dim, kind, size):
+    """Keys of one size and queries of either sign: equal scores of 2^33 and more are a mean over the values; with some keys half as
+    large, over the larger scores alone."""
+    cache = make_cache(torch, cq, bits, n // 16 + 1, 1, 16, dim, cols=False, alpha=1.0, seed=44)
+    table, lens = make_table(torch, cache, [n], seed=44)
+    pos = torch.arange(n)
+    at = table[0].cpu().long()[pos // 16] * 16 + pos % 16
+    dtype = getattr(torch, kind)
+    Q = torch.full((1, 1, group, dim), size, dtype=dtype, device="cuda")
+    Q[:, :, 1::2] = -size
+    Q[:, :, 2] /= 3.0
+    V = torch.randn((n, 1, dim), generator=torch.Generator().manual_seed(n)).to(dtype).cuda()
+    half = torch.zeros(n, dtype=torch.bool)
+    for part in (None, slice(0, 3), slice(n - 9, n), slice(0, n, 2)):
+        if part is not None:
+            half[part] = True
+        K = torch.full((n, 1, dim), size, dtype=dtype)
+        K[half] /= 2.0
+        cq.crossquant_cache_write(cache, K.cuda(), V, at.to(torch.int32).cuda())
+        codes, scale, _ = places(torch, cache, "v")
+        v = codes[at, 0] * scale[at, 0, None]
+        out = cq.crossquant_cache_attention(cache, Q, table, lens)[0, 0].double()
+        large = v[~half].mean(0)
+        small = v[half].mean(0) if part is not None else large
+        for h in range(group):
+            ref = small if h % 2 else large
+            # (every weight is the same: its two numbers, n sums of values and of ones, one quotient)
+            tol = ROUND[kind] * ref.abs() + (1 + ROUND[kind]) * (2.0 ** -21 + 2 * n * 2.0 ** -24) * v.abs().mean(0) * n / max(1, int((half if h % 2 and part is not None else ~half).sum())) + 2.0 ** -25
+            assert ((out[h] - ref).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits,n,group,dim", [(8, 60, 4, 128), (4, 900, 20, 64)])
+@pytest.mark.parametrize("k_size,q_size", [(1e34, 1e-29), (1e-30, 1e30)])
+def test_scores_of_huge_keys_and_tiny_queries(cq, torch, bits, n, group, dim, k_size, q_size):
+    """Scores of ordinary size from factors at the ends of bfloat16."""
+    cache = make_cache(torch, cq, bits, n // 16 + 1, 2, 16, dim, cols=False, alpha=1.0, seed=45)
+    table, lens = make_table(torch, cache, [n], seed=45)
+    pos = torch.arange(n)
+    at = table[0].cpu().long()[pos // 16] * 16 + pos % 16
+    g = torch.Generator().manual_seed(n)
+    K, V = (torch.randn((n, 2, dim), generator=g) for _ in range(2))
+    cq.crossquant_cache_write(cache, (K * k_size).bfloat16().cuda(), V.bfloat16().cuda(), at.to(torch.int32).cuda())
+    Q = (torch.randn((1, 1, 2 * group, dim), generator=g) * q_size).bfloat16().cuda()
+    check_attention(torch, cq, cache, Q, table, lens, scale=0.3 / (k_size * q_size))
 
 
 # ---- the largest calls ---------------------------------------------------------------------------------------------
