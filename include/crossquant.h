@@ -392,6 +392,7 @@ int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T
  *   as they are.
  * Scores, softmax statistics and sums are binary32.  The weights of the values, softmax weight times the value row's factor, are two
  *   binary16 numbers each: 22 bits down to 2^-16 of the row's largest product of the two, and never off by more than 2^-38 of that.
+ *   Values are summed before they are divided by the weights' sum: below 2^96 they stay in binary32 at every length.
  */
 int64_t crossquant_cache_attention_workspace(const cq_cache *cache, int64_t B, int64_t S, int64_t q_heads, int64_t max_length);
 int crossquant_cache_attention(const cq_cache *cache, const void *Q, int64_t q_batch_stride, int64_t q_token_stride,

@@ -13,11 +13,12 @@
 // operand is q' as 16-bit fixed-point number relative to the row's largest |q'|: two signed digits, two products, an exact 32-bit
 // sum (256 high + low: at most 256 * 127 * 32512 < 2^31), off by at most 1.6e-5 (half of 1 / 32512) of that largest.  Against codes turned into
 // binary16: no conversion of K at all, at the same matrix time.  INT4 codes enter as 16 times their value (a mask or a shift).
-// Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) in units of 2^-14 R, R the row's
-// largest w so far up to a power of two.  R shrinks with the weights as m grows, so that the sums, in units of it too, need no
-// rescaling then; a larger w takes a new R and rescales them.  The 22 bits reach 16 binades below the largest w, the units of the second
-// number 38.  (With R from the largest a, whatever its position's score, as here before, a value 2^30 times the others that no query
-// attends to took all but 8 bits of them: 64 x 1024-8192 125.3 us now and 124.4 then, 2 x 131072 INT4 62.7 and 61.)
+// Values: weights w_p = 2^(z_p - m) a_p become two binary16 numbers (rounded, and what is left: 22 bits) in units of R / 65504, R the
+// row's largest w so far up to a power of two and two binades.  R shrinks with the weights as m grows, so that the sums, in units of it
+// too, need no rescaling then; a larger w takes a new R and rescales them.  The 22 bits reach 16 binades below the largest w, the units of
+// the second number 38.  (With R from the largest a, whatever its position's score, a value 2^30 times the others that no query attends to
+// took all but 8 bits of them.  Without the two binades some row of a wave takes a new R in most tiles of a stretch: 2 x 131072 INT4
+// 62 us, with them 60.3; 64 x 1024-8192, INT4, 86.2 and 85.6.)
 // Codes become binary16 exactly (as subnormal numbers, and from there in one fused step).  With one number a weight the result was off by sqrt(2) times what its
 // own rounding to binary16 costs; the second product is in the shadow of the loads.  Sums, m and the sum of 2^(z - m) are binary32.
 //
@@ -40,7 +41,8 @@ constexpr int kWaves = 4;
 constexpr int kSub = 2;                                    // subtiles of 16 positions that a wave works on at a time
 constexpr int kTile = 16 * kSub, kBlockStep = kWaves * kTile;
 constexpr float kDigits = 32512.0f;                        // 127 * 256
-constexpr float kWeightTop = 16384.0f;                     // 2^14
+constexpr float kWeightTop = 65504.0f;                     // binary16's largest
+constexpr uint32_t kHeadroom = 2;                          // binades that R leaves above the product it is taken from
 constexpr float kSmallest = 7.888609052210118e-31f;        // 2^-100: queries below count as zero, and R is no smaller
 
 struct Args {
@@ -385,7 +387,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
             const float keep = __builtin_amdgcn_exp2f(m[mr] - ref);
             m[mr] = top;
             l[mr] *= keep;
-            float w[kSub][4], w_top = 0.0f;
+            float w[kSub][4], w_top = kSmallest;
 #pragma unroll
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
@@ -403,18 +405,19 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
                     }
                     w_top = fmaxf(w_top, fmaxf(w[t][r], w[t][r + 1]));
                 }
-            // Sums so far shrink with R as m grows; a larger product, or an R about to leave the normal numbers, takes a new power of two.
+            // Sums so far shrink with R as m grows; a larger product (or an R below 2^-100) takes a new power of two.
             R[mr] *= keep;
-            if (__any((w_top >= R[mr]) | (R[mr] < kSmallest))) {
+            if (__any(w_top >= R[mr])) {
                 w_top = max_groups(w_top);
-                const bool more = (w_top >= R[mr]) | (R[mr] < kSmallest);
-                const float R_new = more ? fmaxf(kSmallest, __uint_as_float((__float_as_uint(w_top) & 0x7F800000u) + 0x00800000u)) : R[mr];
-                const float shrink = R[mr] / R_new;
+                const bool more = w_top >= R[mr];
+                // (2^126 at most, which is above every factor that a row of numbers can have)
+                const uint32_t R_bits = min((__float_as_uint(w_top) & 0x7F800000u) + (kHeadroom + 1) * 0x00800000u, 0x7E800000u);
+                const float shrink = more ? R[mr] * __uint_as_float(0x7F000000u - R_bits) : 1.0f;     // (times 1 / R_new)
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[mr][i][r] *= shrink;
-                R[mr] = R_new;
+                R[mr] = more ? __uint_as_float(R_bits) : R[mr];
             }
             const float to_weight = kWeightTop * __builtin_amdgcn_rcpf(R[mr]);
 #pragma unroll
@@ -472,7 +475,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
 #pragma unroll
     for (int mr = 0; mr < MR; ++mr) {
         __syncthreads();                                   // (what the last piece or rows left has been read)
-        const float sum = sum_groups(l[mr]);
+        const float sum = sum_groups(l[mr]), unit = R[mr] * (16384.0f / kWeightTop);          // (2^-14 a code)
         if (grp == 0) {
             sh.ml[wave][fr][0] = m[mr];
             sh.ml[wave][fr][1] = sum;
@@ -483,7 +486,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
 #pragma unroll
             for (int i = 0; i < kOut; i += 4)
                 *reinterpret_cast<float4*>(&sh.o[wave][fr][kOut * (4 * grp + r) + i]) =
-                    make_float4(o[mr][i][r] * R[mr], o[mr][i + 1][r] * R[mr], o[mr][i + 2][r] * R[mr], o[mr][i + 3][r] * R[mr]);
+                    make_float4(o[mr][i][r] * unit, o[mr][i + 1][r] * unit, o[mr][i + 2][r] * unit, o[mr][i + 3][r] * unit);
         __syncthreads();
         constexpr int kCols = DIM / 16;                    // channels a thread joins
         const int row = threadIdx.x / 16, d0 = threadIdx.x % 16 * kCols, in_tile = 16 * mr + row;

@@ -140,8 +140,8 @@ def weight_tolerance(torch, cache, Q, table, lengths, scale, max_length, ref):
     A score z passes seven roundings to binary32 (the integer product, the key's factor, three of the row's factor, the product, the
     exponent), each 2^-24 of it: dz = 2^-21 |z|, in numerator and denominator.  The exponential, its product with the value's factor and
     the weights' common factor (reciprocal included) are 6 times 2^-23; the two numbers of a weight keep it to 2^-22 of itself, and to
-    2^-25 of the unit 2^-14 R where they are subnormal, R at most twice the largest product of a softmax weight and a factor of the
-    row.  Sums are binary32: a rounding (counted twice: the matrix instruction may truncate) for each value that is not zero, the
+    2^-25 of the unit R / 65504 where they are subnormal, R at most eight times the largest product of a softmax weight and a factor of
+    the row: 2^-38 of that.  Sums are binary32: a rounding (counted twice: the matrix instruction may truncate) for each value that is not zero, the
     8 waves, the pieces, and the factors that join them."""
     B, S, HQ, D = Q.shape
     H, page, q_max = cache.heads, cache.page_size, 127 if cache.bits == 8 else 7
