@@ -374,8 +374,8 @@ int crossquant_cache_write(const cq_cache *cache, const void *K, int64_t k_token
 int crossquant_cache_read(const cq_cache *cache, const int32_t *slots, int64_t T, void *K, void *V, int type, void *stream);
 
 /*
- * Attention of the last S tokens of B sequences over the cache (decode: S = 1, or a few drafted tokens), whose keys and values are
- * in the cache already:
+ * Attention of the last S tokens of B sequences over the cache (made for decode: S = 1, or a few drafted tokens), whose keys and values
+ * are in the cache already:
  *   out[b][s][h] = sum_p softmax_p(scale * q . k_p) v_p over the positions p < min(lengths[b] - (S - 1 - s), max_length)
  * with k_p, v_p of head h / (q_heads / heads) in binary32 from the codes.  Position p of sequence b is place p % page_size of page
  * page_table[b][p / page_size].  A row that sees no position (lengths[b] too small, or negative) is zero, whatever its query holds.  Positions

@@ -7,7 +7,7 @@
 // fourth tile of 32 positions, each with a running maximum, sum and output of its own, which meet at the piece's end.  A pair that lies in one
 // stretch is done then; pieces of others go to the workspace and a second kernel joins them.
 // (64 sequences of 1024 to 8192 positions, 512 pairs: with the pairs' maximum length cut into a fixed number of blocks 175 us at best, 135 so; with
-// what came later 125, 5.1 TB/s; 2 sequences of 73728 and 131072 positions, INT4, 8 heads: 57 us, 3.9 TB/s.)
+// what came later 125, 5.1 TB/s; 2 sequences of 73728 and 131072 positions, INT4, 8 heads: 57 to 60 us, 3.7 to 3.9 TB/s.)
 //
 // Scores: the column factors go into the query, q' = q b, and the codes into the INT8 matrix instruction as they are.  The other
 // operand is q' as 16-bit fixed-point number relative to the row's largest |q'|: two signed digits, two products, an exact 32-bit

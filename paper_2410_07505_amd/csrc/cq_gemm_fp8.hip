@@ -295,7 +295,7 @@ gemm_fp8_kernel(const int8_t* __restrict__ qx, const float* __restrict__ x_scale
 //     and the first of step k + 2 are requested in step k, into the place that step k - 1 left and the one that was free;
 //   token scales: three slots of 1 KiB.
 // Measured (4096 x 8192 x 28672): all requests of a step at once behind the barrier, two whole slots 988 us; two a product, by all
-// waves, 857; this form 790 to 810, 780 with whole-line stores, 2.45 PFLOP/s.  With operands of zeros it took 690: the difference is the
+// waves, 857; this form 790 to 810, with whole-line stores 777 to 806 over cards, 2.39 to 2.47 PFLOP/s.  With operands of zeros it took 690: the difference is the
 // clock under power, 1.8 GHz.  Without the requests of all steps but the first it would take 666 (zeros: 568), without the additions 723.
 // Matrix instructions alone from registers reach 4.5 PFLOP/s; what remains are the instructions a wave has to issue between
 // them (reads of fragments, additions, requests).
