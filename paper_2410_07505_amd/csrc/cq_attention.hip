@@ -252,8 +252,8 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
                 x[c + e] = a.bf16 ? __uint_as_float(h << 16) : h2f(h);
             }
             if (a.k_col) {
-                const float4 lo = *reinterpret_cast<const float4*>(a.k_col + head * DIM + d);
-                const float4 hi = *reinterpret_cast<const float4*>(a.k_col + head * DIM + d + 4);
+                const float4 lo = *reinterpret_cast<const float4*>(a.k_col + (int64_t)head * DIM + d);
+                const float4 hi = *reinterpret_cast<const float4*>(a.k_col + (int64_t)head * DIM + d + 4);
                 const float b[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[c + e] *= b[e];
@@ -507,7 +507,7 @@ __device__ __forceinline__ void attention_piece(const Args& a, Shared<DIM, W>& s
         }
         if (a.v_col) {
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) acc[c] *= a.v_col[head * DIM + d0 + c];
+            for (int c = 0; c < kCols; ++c) acc[c] *= a.v_col[(int64_t)head * DIM + d0 + c];
         }
         if (piece < 0) {
             const int rr = row0 + in_tile, s = rr / a.group, h = head * a.group + rr % a.group;

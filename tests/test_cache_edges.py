@@ -419,3 +419,30 @@ def test_calls_of_more_than_sixteen_million_rows(cq, torch, B, S, heads, group, 
     for b in range(0, B, size):
         seen = (lens[b:b + size, None] - (S - 1 - torch.arange(S, device="cuda"))).clamp(min=0)
         assert torch.equal(out[b:b + size].view(torch.int16), want[seen].view(torch.int16))
+
+
+@pytest.mark.gpu
+def test_column_factors_behind_two_to_the_31(cq, torch):
+    """More heads than 32-bit offsets into their factors reach (about 60 GiB)."""
+    heads, dim, page, few = (1 << 23) + 3, 256, 16, 5
+    small = make_cache(torch, cq, 4, 1, few, page, dim, alpha=0.3, seed=71)
+    tensors, cols = [], []
+    for n in "kv":
+        codes = torch.zeros((1, heads, page, dim // 2), dtype=torch.uint8, device="cuda")
+        scale = torch.zeros((1, heads, page), device="cuda")
+        col = torch.zeros((heads, dim), device="cuda")
+        for t, name in ((codes, "_codes"), (scale, "_scale")):
+            t[:, -few:] = getattr(small, n + name)
+        col[-few:] = getattr(small, n + "_col")
+        tensors += [codes, scale]
+        cols.append(col)
+    cache = cq.crossquant_cache(*tensors, 4, alpha=0.3, k_col=cols[0], v_col=cols[1])
+    table, lens = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1,), 13, dtype=torch.int32, device="cuda")
+    q = queries(torch, 1, 1, few, dim, "bfloat16")
+    Q = torch.zeros((1, 1, heads, dim), dtype=torch.bfloat16, device="cuda")
+    Q[:, :, -few:] = q
+    out = cq.crossquant_cache_attention(cache, Q, table, lens)
+    assert torch.equal(out[:, :, -few:], cq.crossquant_cache_attention(small, q, table, lens))
+    assert not out.view(torch.int64)[:, :, :-few].any()
+    del cache, tensors, cols, Q, out, codes, scale, col, t
+    torch.cuda.empty_cache()
